@@ -348,6 +348,122 @@ int lopa_window_update(lopa_window* win, int32_t* tokens, float* conf, int32_t* 
  * nothing and set win->error = 1. */
 int lopa_window_commit(lopa_kv* kv, const int32_t* winner, lopa_window* win, void* stream);
 
+/* ------------------------------------------------ serving: paged cache */
+
+/* Operators for callers that keep the K / V of many sequences in pages of their
+ * own (several requests, or the branches of one prefix sharing its pages), next
+ * to the static one-sequence cache of a lopa_kv. Nothing here needs a model
+ * handle or allocates device memory: every array is the caller's, on the current
+ * device. Two calls may run at once on two streams if they share no array that
+ * one of them writes (a workspace among them). */
+
+/* Element types of the serving operators. */
+enum { LOPA_BF16 = 0, LOPA_F16 = 1, LOPA_F32 = 2 };
+
+/* One layer's pages (host struct): K and V are [n_pages][kv_heads][page_size]
+ * [head_dim] each, contiguous, 16-byte aligned, of type LOPA_BF16 or LOPA_F16;
+ * page_size is 16, 32, 64, 128 or 256, head_dim 64 or 128. */
+typedef struct lopa_pages {
+  void* k;
+  void* v;
+  int32_t n_pages;
+  int32_t kv_heads;
+  int32_t page_size;
+  int32_t head_dim;
+  int32_t dtype;
+} lopa_pages;
+
+/* A batch of sequences whose newest tokens are rows of the calls below (host
+ * struct, device arrays). Sequence s has the rows q_start[s] .. q_start[s+1] - 1
+ * (q_start[n_seq + 1], not decreasing, within [0, rows]) and kv_len[s] tokens with
+ * them: row i of its n is its position kv_len[s] - n + i. Position p lies in slot
+ * p % page_size of page table[s * table_ld + p / page_size]. A table entry outside
+ * [0, n_pages) is a page that is not there: nothing is written to it and no row
+ * sees a key of it. Entries past a sequence's last page are not used. Rows outside
+ * every sequence are left as they are. At most 65535 sequences, 2^24 rows, table_ld
+ * * page_size < 2^30. */
+typedef struct lopa_paged_batch {
+  const int32_t* table;
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  int32_t n_seq;
+  int32_t table_ld;
+  int32_t rows;
+} lopa_paged_batch;
+
+/* New tokens enter the cache. q [rows][heads][head_dim], k and v
+ * [rows][kv_heads][head_dim] of the pages' type, rows ld_q / ld_k / ld_v elements
+ * apart (so the three may lie in one packed projection output), heads contiguous;
+ * pointers 16-byte aligned, row strides multiples of 8.
+ * Every query and key head x of a row at position p:
+ *   y = x / sqrt(mean(x^2) + eps) * w   w = q_norm / k_norm [head_dim] of the same
+ *                                       type; NULL: y = x, no norm
+ *   out_j       = y_j cos(a_j) - y_{j+h} sin(a_j)      h = head_dim / 2, j < h,
+ *   out_{j+h}   = y_{j+h} cos(a_j) + y_j sin(a_j)      a_j = p rope_theta^(-j/h)
+ * (rope_theta = 0: no rotation), in fp32 with the angle reduced in fp64, rounded
+ * once. Queries go to q_out [rows][heads][head_dim] (rows ld_out apart; q itself is
+ * allowed), keys and the values as they are to their pages. Two rows that name the
+ * same slot race. */
+int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, int32_t heads,
+                      const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
+                      int64_t ld_v, const void* q_norm, const void* k_norm, float eps,
+                      float rope_theta, void* q_out, int64_t ld_out, void* stream);
+
+/* Attention of the batch's rows over their pages (which hold the rows' own K and V
+ * already). Query head g of a row at position p reads K / V head g / (heads /
+ * kv_heads) at the positions j of its sequence with
+ *   block = 0: j < kv_len            full
+ *   block = 1: j <= p                causal
+ *   block = c: j < (p / c + 1) c     block-causal: its own block and all before
+ * (and j < kv_len always).
+ *   s_j = scale q . K_j, or softcap tanh(scale q . K_j / softcap) if softcap > 0
+ *   out = sum_j softmax(s)_j V_j;  lse = ln sum_j exp(s_j) (fp32 [rows][heads], or
+ *   NULL)
+ * A row that sees no key gives zeros and lse = -inf. Keys that a row does not see
+ * have no part in it, whatever they hold (NaN and infinities too). q and out
+ * [rows][heads][head_dim] of the pages' type as in lopa_paged_append. Products of
+ * that type are summed in fp32; the softmax is fp32, its numerators are rounded to
+ * the type for the product with V.
+ * max_rows and max_len bound the rows and the kv_len of a sequence; the launch is
+ * laid out for them, so a captured call serves every batch within them. A sequence
+ * past either bound is left out (its rows stay as they are).
+ * workspace (device, 16-byte aligned): at least the bytes that
+ * lopa_paged_attention_workspace gives for the same sizes, NULL if that is 0.
+ * Errors: LOPA_ECAPACITY for max_len > table_ld * page_size, LOPA_ESHAPE for a
+ * layout the kernels do not take or too small a workspace. */
+int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch, int32_t heads,
+                         int32_t max_rows, int32_t max_len, const void* q, int64_t ld_q,
+                         int32_t block, float scale, float softcap, void* out, int64_t ld_out,
+                         float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+/* Bytes of workspace (host only, no HIP call), or a negative status. */
+int64_t lopa_paged_attention_workspace(int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                       int32_t n_seq, int32_t rows, int32_t max_rows,
+                                       int32_t max_len);
+
+/* What rows of logits say: x = logits[r][0 .. vocab) of type LOPA_BF16, LOPA_F16 or
+ * LOPA_F32, rows ld >= vocab elements apart. Conf of the verify forward is
+ * exp(top_logprobs[r][0]).
+ *   logprob[r] = x_t - lse, t = tokens[r]; 0 for t < 0 (no token), NaN for
+ *                t >= vocab; lse = ln sum_i exp(x_i)
+ *   entropy[r] = -sum_i p_i ln p_i, p_i = exp(x_i - lse) (nats)
+ *   top_ids / top_logprobs [rows][n_top]: the tokens of largest x and their
+ *                log probabilities, largest first, lowest token on ties
+ * exclude in [0, vocab): that token (the mask token) is outside the support: -inf
+ * as a given token, never among the top ones; -1: none. Tokens of logit -inf have
+ * no part either; places of the top list that are left have id -1 and -inf. A row
+ * in which nothing is left has entropy 0 and lse -inf (logprob -inf). A row with a
+ * NaN or +inf has no distribution: logprob (of t >= 0), entropy and top_logprobs
+ * are NaN and its ids -1.
+ * logprob (with tokens), entropy and the top list (both arrays) may be NULL each.
+ * 1 <= vocab <= 2^24, 0 <= n_top <= LOPA_MAX_TOP. fp32 throughout. */
+#define LOPA_MAX_TOP 32
+int lopa_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int32_t rows,
+                        int32_t vocab, int32_t exclude, const int32_t* tokens, int32_t n_top,
+                        float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+/* Bytes of workspace (host only, no HIP call), or a negative status. */
+int64_t lopa_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top);
+
 /* ---------------------------------------------------------- inspection */
 
 /* Copy cache rows [start, start+len) of one layer to k_dst, v_dst (device,

@@ -9,6 +9,12 @@ the stream. The functions keep the C names:
     lopa_branch_confidence_select  Eq. 2 scores, argmax, next state (Sec. 3.2 logit reuse)
     lopa_commit_kv                 winner K/V -> static cache (Sec. 3.4)
 
+and, for callers that keep the K / V of many sequences in pages of their own:
+
+    lopa_paged_append              head norms + rotation of new rows, K / V to their pages
+    lopa_paged_attention           a ragged batch's rows over their pages
+    lopa_token_logprobs            log probability, entropy and top tokens of rows of logits
+
 Importing this module loads liblopa.so built in-tree by build.py (or
 __graft_entry__.build()); there is no fallback: a missing library raises.
 """
@@ -18,10 +24,11 @@ import ctypes as C
 
 import torch
 
-from ._abi import (EXPORTS, LIB_PATH, LOPA_ECAPACITY, LOPA_EHIP, LOPA_EINVAL, LOPA_ENOMEM,  # noqa: F401
-                   LOPA_ESHAPE, LOPA_OK, MAX_BLOCK, MAX_ROWS, METRIC_LOWEST_SEGMENT, METRIC_MEAN,
-                   METRIC_WINDOW_MIN, PRECISIONS, PROF_KINDS, WINDOW_MAX_BLOCKS, LopaError, lib,
-                   lopa_layer_weights, lopa_model_cfg, lopa_weight_ptrs, lopa_window)
+from ._abi import (EXPORTS, LIB_PATH, LOPA_BF16, LOPA_ECAPACITY, LOPA_EHIP, LOPA_EINVAL,  # noqa: F401
+                   LOPA_ENOMEM, LOPA_ESHAPE, LOPA_F16, LOPA_F32, LOPA_OK, MAX_BLOCK, MAX_ROWS, MAX_TOP,
+                   METRIC_LOWEST_SEGMENT, METRIC_MEAN, METRIC_WINDOW_MIN, PRECISIONS, PROF_KINDS,
+                   WINDOW_MAX_BLOCKS, LopaError, lib, lopa_layer_weights, lopa_model_cfg,
+                   lopa_paged_batch, lopa_pages, lopa_weight_ptrs, lopa_window)
 
 
 def _check(status: int):
@@ -262,6 +269,153 @@ def lopa_window_update(win, tokens, conf, pred, out_tokens, stream=None):
 def lopa_window_commit(kv: KV, winner, win, stream=None):
     _check(lib.lopa_window_commit(kv.handle, _ptr(winner, I32, "winner"), _ptr(win, I32, "win"),
                                   _stream(stream)))
+
+
+# ------------------------------------------------------ serving: paged cache
+_DTYPES = {torch.bfloat16: LOPA_BF16, torch.float16: LOPA_F16, torch.float32: LOPA_F32}
+
+
+def _one_device(tensors: dict, stream):
+    """The device that holds every tensor (None: not given), and the stream there."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch tensor")
+        if t.device.type != "cuda":
+            raise ValueError(f"{name}: must be a device tensor")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"{name}: on {t.device}, the others on {dev}")
+        dev = t.device
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif hasattr(stream, "device") and stream.device != dev:
+        raise ValueError(f"stream of {stream.device}, the tensors on {dev}")
+    return dev, _stream(stream)
+
+
+def _rows(t, shape, dtype, name):
+    """[rows][heads][head_dim] with contiguous heads: its pointer and row stride."""
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    n, h, d = shape
+    if t.numel() and (t.stride(2) != 1 or (h > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return C.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else h * d
+
+
+def _paged(k_pages, v_pages, table, q_start, kv_len, rows):
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
+        raise ValueError("k_pages, v_pages: expected one shape [pages][kv_heads][page_size][head_dim]")
+    if k_pages.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError(f"k_pages: expected bfloat16 or float16, got {k_pages.dtype}")
+    n_seq = kv_len.numel()
+    if table.dim() != 2 or table.shape[0] != n_seq or q_start.numel() != n_seq + 1:
+        raise ValueError("table, q_start, kv_len: expected [n_seq][pages], [n_seq + 1] and [n_seq]")
+    n, hkv, ps, d = k_pages.shape
+    pages = lopa_pages(_ptr(k_pages, k_pages.dtype, "k_pages"), _ptr(v_pages, k_pages.dtype, "v_pages"),
+                       n, hkv, ps, d, _DTYPES[k_pages.dtype])
+    batch = lopa_paged_batch(_ptr(table, I32, "table"), _ptr(q_start, I32, "q_start"),
+                             _ptr(kv_len, I32, "kv_len"), n_seq, table.shape[1], rows)
+    return pages, batch
+
+
+def lopa_paged_append(k_pages, v_pages, table, q_start, kv_len, q, k, v, q_norm, k_norm, eps,
+                      rope_theta, q_out, stream=None):
+    """q [rows][heads][d], k and v [rows][kv_heads][d] (row strides are free, so views of a
+    packed projection output do); q_norm / k_norm [d] or None; q_out like q."""
+    dev, st = _one_device(dict(k_pages=k_pages, v_pages=v_pages, table=table, q_start=q_start,
+                               kv_len=kv_len, q=q, k=k, v=v, q_norm=q_norm, k_norm=k_norm,
+                               q_out=q_out), stream)
+    if q.dim() != 3:
+        raise ValueError("q: expected [rows][heads][head_dim]")
+    rows, heads = q.shape[:2]
+    pages, batch = _paged(k_pages, v_pages, table, q_start, kv_len, rows)
+    t, hkv, d = k_pages.dtype, k_pages.shape[1], k_pages.shape[3]
+    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+        if w is not None and tuple(w.shape) != (d,):
+            raise ValueError(f"{name}: expected shape {(d,)}, got {tuple(w.shape)}")
+    qp, ldq = _rows(q, (rows, heads, d), t, "q")
+    kp, ldk = _rows(k, (rows, hkv, d), t, "k")
+    vp, ldv = _rows(v, (rows, hkv, d), t, "v")
+    op, ldo = _rows(q_out, (rows, heads, d), t, "q_out")
+    with torch.cuda.device(dev):
+        _check(lib.lopa_paged_append(C.byref(pages), C.byref(batch), heads, qp, ldq, kp, ldk, vp, ldv,
+                                     _ptr(q_norm, t, "q_norm"), _ptr(k_norm, t, "k_norm"), float(eps),
+                                     float(rope_theta), op, ldo, st))
+
+
+def lopa_paged_attention_workspace(heads, kv_heads, head_dim, n_seq, rows, max_rows, max_len) -> int:
+    """Bytes of workspace that lopa_paged_attention needs for these sizes."""
+    n = lib.lopa_paged_attention_workspace(heads, kv_heads, head_dim, n_seq, rows, max_rows, max_len)
+    if n < 0:
+        _check(n)
+    return n
+
+
+def lopa_paged_attention(q, k_pages, v_pages, table, q_start, kv_len, max_rows, max_len, block, scale,
+                         softcap, out, lse=None, workspace=None, stream=None):
+    """q and out [rows][heads][d] (free row strides); block 0 full, 1 causal, c block-causal;
+    lse [rows][heads] fp32 or None; workspace: a contiguous tensor of the bytes that
+    lopa_paged_attention_workspace gives, or None."""
+    dev, st = _one_device(dict(q=q, k_pages=k_pages, v_pages=v_pages, table=table, q_start=q_start,
+                               kv_len=kv_len, out=out, lse=lse, workspace=workspace), stream)
+    if q.dim() != 3:
+        raise ValueError("q: expected [rows][heads][head_dim]")
+    rows, heads = q.shape[:2]
+    pages, batch = _paged(k_pages, v_pages, table, q_start, kv_len, rows)
+    t, d = k_pages.dtype, k_pages.shape[3]
+    qp, ldq = _rows(q, (rows, heads, d), t, "q")
+    op, ldo = _rows(out, (rows, heads, d), t, "out")
+    if lse is not None and tuple(lse.shape) != (rows, heads):
+        raise ValueError(f"lse: expected shape {(rows, heads)}, got {tuple(lse.shape)}")
+    size = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    with torch.cuda.device(dev):
+        _check(lib.lopa_paged_attention(C.byref(pages), C.byref(batch), heads, max_rows, max_len, qp, ldq,
+                                        block, float(scale), float(softcap), op, ldo,
+                                        _ptr(lse, F32, "lse"), _ptr(workspace, None, "workspace"), size,
+                                        st))
+
+
+def lopa_token_logprobs_workspace(rows, vocab, n_top) -> int:
+    """Bytes of workspace that lopa_token_logprobs needs for these sizes."""
+    n = lib.lopa_token_logprobs_workspace(rows, vocab, n_top)
+    if n < 0:
+        _check(n)
+    return n
+
+
+def lopa_token_logprobs(logits, tokens, exclude, logprob=None, entropy=None, top_ids=None,
+                        top_logprobs=None, workspace=None, stream=None):
+    """logits [rows][vocab] of bfloat16, float16 or float32 (free row stride); tokens [rows] with
+    logprob [rows]; entropy [rows]; top_ids and top_logprobs [rows][n]; each output may be None.
+    exclude: a token outside the support, or -1."""
+    dev, st = _one_device(dict(logits=logits, tokens=tokens, logprob=logprob, entropy=entropy,
+                               top_ids=top_ids, top_logprobs=top_logprobs, workspace=workspace), stream)
+    if logits.dim() != 2 or logits.dtype not in _DTYPES:
+        raise TypeError("logits: expected [rows][vocab] of bfloat16, float16 or float32")
+    rows, vocab = logits.shape
+    if logits.numel() and logits.stride(1) != 1:
+        raise ValueError("logits: a row must be contiguous")
+    n = top_ids.shape[-1] if top_ids is not None else 0
+    for name, t, shape in (("tokens", tokens, (rows,)), ("logprob", logprob, (rows,)),
+                           ("entropy", entropy, (rows,)), ("top_ids", top_ids, (rows, n)),
+                           ("top_logprobs", top_logprobs, (rows, n))):
+        if t is not None and tuple(t.shape) != shape:
+            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if n == 0:
+        top_ids = top_logprobs = None
+    size = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    with torch.cuda.device(dev):
+        _check(lib.lopa_token_logprobs(C.c_void_p(logits.data_ptr()), _DTYPES[logits.dtype],
+                                       logits.stride(0) if rows > 1 else vocab, rows, vocab, exclude,
+                                       _ptr(tokens, I32, "tokens"), n, _ptr(logprob, F32, "logprob"),
+                                       _ptr(entropy, F32, "entropy"), _ptr(top_ids, I32, "top_ids"),
+                                       _ptr(top_logprobs, F32, "top_logprobs"),
+                                       _ptr(workspace, None, "workspace"), size, st))
 
 
 from .decoder import Decoder, WindowDecoder  # noqa: E402,F401

@@ -13,6 +13,8 @@ LIB_PATH = os.path.join(_HERE, "liblopa.so")
 
 LOPA_OK, LOPA_EINVAL, LOPA_ESHAPE, LOPA_ECAPACITY, LOPA_EHIP, LOPA_ENOMEM = 0, -1, -2, -3, -4, -5
 MAX_BLOCK, MAX_ROWS, WINDOW_MAX_BLOCKS = 256, 2048, 16
+LOPA_BF16, LOPA_F16, LOPA_F32 = 0, 1, 2
+MAX_TOP = 32
 
 
 class LopaError(RuntimeError):
@@ -46,6 +48,16 @@ class lopa_weight_ptrs(C.Structure):
                 ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class lopa_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [
+        (n, C.c_int32) for n in ("n_pages", "kv_heads", "page_size", "head_dim", "dtype")]
+
+
+class lopa_paged_batch(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("table", "q_start", "kv_len")] + [
+        (n, C.c_int32) for n in ("n_seq", "table_ld", "rows")]
+
+
 EXPORTS = ["lopa_model_create", "lopa_model_create_ex", "lopa_model_destroy", "lopa_kv_create", "lopa_kv_destroy",
            "lopa_strerror", "lopa_last_error", "lopa_build_branches", "lopa_build_branches_window",
            "lopa_verify_forward", "lopa_prefill",
@@ -54,7 +66,8 @@ EXPORTS = ["lopa_model_create", "lopa_model_create_ex", "lopa_model_destroy", "l
            "lopa_kv_read_staging", "lopa_debug_hidden",
            "lopa_kv_set_block_causal", "lopa_kv_profile",
            "lopa_kv_profile_read", "lopa_verify_forward_noalloc", "lopa_window_init",
-           "lopa_window_update", "lopa_window_commit"]
+           "lopa_window_update", "lopa_window_commit", "lopa_paged_append", "lopa_paged_attention",
+           "lopa_paged_attention_workspace", "lopa_token_logprobs", "lopa_token_logprobs_workspace"]
 METRIC_MEAN, METRIC_WINDOW_MIN, METRIC_LOWEST_SEGMENT = 0, 1, 2
 PRECISIONS = {"bf16": 0, "fp8_mlp": 1, "fp8": 2}
 PROF_KINDS = ["qkv", "attn", "oproj", "gateup", "down", "lmhead", "norm", "merge"]
@@ -64,7 +77,8 @@ def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python paper_2512_16229_amd/build.py`")
     lib = C.CDLL(LIB_PATH)
-    P, I32, F32 = C.c_void_p, C.c_int32, C.c_float
+    P, I32, I64, F32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+    PAGES, BATCH = C.POINTER(lopa_pages), C.POINTER(lopa_paged_batch)
     sig = {
         "lopa_model_create": (C.c_int, [C.POINTER(lopa_model_cfg), C.POINTER(lopa_weight_ptrs), P,
                                         C.POINTER(C.c_void_p)]),
@@ -92,6 +106,13 @@ def _load():
         "lopa_kv_profile": (C.c_int, [P, I32]),
         "lopa_kv_profile_read": (C.c_int, [P, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
         "lopa_verify_forward_noalloc": (C.c_int, [P, P, I32, P, I32, I32, P, P, P]),
+        "lopa_paged_append": (C.c_int, [PAGES, BATCH, I32, P, I64, P, I64, P, I64, P, P, F32, F32, P,
+                                        I64, P]),
+        "lopa_paged_attention": (C.c_int, [PAGES, BATCH, I32, I32, I32, P, I64, I32, F32, F32, P, I64,
+                                           P, P, I64, P]),
+        "lopa_paged_attention_workspace": (I64, [I32] * 7),
+        "lopa_token_logprobs": (C.c_int, [P, I32, I64, I32, I32, I32, P, I32, P, P, P, P, P, I64, P]),
+        "lopa_token_logprobs_workspace": (I64, [I32] * 3),
         "lopa_window_init": (C.c_int, [P, P, P, P, I32, I32, I32, I32, I32, C.c_double, C.c_double, P]),
         "lopa_window_update": (C.c_int, [P, P, P, P, P, P]),
         "lopa_window_commit": (C.c_int, [P, P, P, P]),

@@ -194,3 +194,56 @@ struct AttnArgs {
   uint32_t* rowmax;
 };
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
+
+// ------------------------------------------------- serving: paged cache
+struct AppendArgs {
+  lopa_pages pages;
+  lopa_paged_batch batch;
+  int heads;
+  const void *q, *k, *v;
+  void* q_out;
+  int64_t ld_q, ld_k, ld_v, ld_out;
+  const void *q_norm, *k_norm;  // null: no norm
+  float eps;
+  int rotate;
+  double turns[64];  // turns per position of pair j < head_dim / 2
+};
+hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
+
+struct PagedPlan {
+  int64_t bytes;  // workspace
+};
+PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
+                               int max_len);
+struct PagedAttnArgs {
+  lopa_pages pages;
+  lopa_paged_batch batch;
+  int heads, max_rows, max_len;
+  const void* q;
+  void* out;
+  int64_t ld_q, ld_out;
+  int block;
+  float scale, softcap;
+  float* lse;
+  float* ws;
+};
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
+
+// ------------------------------------------- serving: log probabilities
+struct LogprobPlan {
+  int64_t bytes;  // workspace
+};
+LogprobPlan logprobs_plan(int rows, int vocab, int n_top);
+struct LogprobArgs {
+  const void* logits;
+  int dtype;
+  int64_t ld;
+  int rows, vocab, exclude;
+  const int32_t* tokens;  // null: none
+  int n_top;
+  float *logprob, *entropy;  // null: not wanted
+  int32_t* top_ids;
+  float* top_logprobs;
+  void* ws;
+};
+hipError_t launch_token_logprobs(const LogprobArgs& a, const LogprobPlan& p, hipStream_t s);
