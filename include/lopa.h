@@ -380,8 +380,8 @@ typedef struct lopa_pages {
  * p % page_size of page table[s * table_ld + p / page_size]. A table entry outside
  * [0, n_pages) is a page that is not there: nothing is written to it and no row
  * sees a key of it. Entries past a sequence's last page are not used. Rows outside
- * every sequence are left as they are. At most 65535 sequences, 2^24 rows, table_ld
- * * page_size < 2^30. */
+ * every sequence are left as they are. At most 65535 sequences, 2^24 rows, fewer
+ * than 2^31 rows x heads, table_ld * page_size < 2^30. */
 typedef struct lopa_paged_batch {
   const int32_t* table;
   const int32_t* q_start;

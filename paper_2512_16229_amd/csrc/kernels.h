@@ -211,7 +211,15 @@ struct AppendArgs {
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
 
 struct PagedPlan {
-  int64_t bytes;  // workspace
+  struct Part {           // one launch: the sequences with m_lo < rows x group <= m_hi
+    int wm;               // 32 wm rows a workgroup
+    int64_t m_lo, m_hi;
+    int64_t slots;        // row tiles' places
+    int splits, chunk;    // key splits of `chunk` keys
+    int64_t ws_bytes;
+  } part[2];
+  int n;
+  int64_t bytes;  // workspace of all parts
 };
 PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
                                int max_len);

@@ -18,3 +18,19 @@ __device__ __forceinline__ int seq_of_row(const int32_t* q_start, int n_seq, int
   }
   return __builtin_amdgcn_readfirstlane(n) - 1;
 }
+
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Asynchronous global -> LDS copy of 16 bytes per lane: lane l copies base + voff(l)
+// to bytes [16 l, 16 l + 16) of the 1 KiB at LDS address `to` (base and `to`
+// wave-uniform). The compiler does not track it: wait_loads() before the data is
+// read. One wait state between the write of M0 and its use.
+__device__ __forceinline__ void copy_to_lds(const void* base, uint32_t voff, uint32_t to) {
+  const uint64_t u = (uint64_t)base;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(voff), "s"(((uint64_t)hi << 32) | lo)
+               : "memory");
+}

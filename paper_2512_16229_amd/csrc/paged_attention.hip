@@ -1,65 +1,629 @@
 // Attention of a ragged batch's rows over paged K / V.
 //
-// One wavefront per (row, query head) walks the row's keys with a running maximum
-// and sum: m' = max(m, s), l' = l 2^(m - m') + 2^(s - m'), o likewise. A lane holds
-// d / 64 dimensions; keys that the row does not see are not read.
+// Mathematics. One pass over the keys with a running reference r and sum l: for a
+// tile of keys, x_j = log2(e) s_j, p_j = 2^(x_j - r), l += sum p_j, o += sum p_j V_j;
+// out = o / l, lse = (r + log2 l) ln 2. r follows the maximum lazily: o and l are
+// rescaled by 2^(r - r') only when some row's maximum has passed r by 2^LIM, so
+// most tiles multiply nothing. p is rounded to the pages' type for the product
+// with V; fp16 has no exponents below 2^-24, so its numerators are kept 2^8 larger.
+//
+// Layout. The rows of a tile are (row, query head) pairs of one sequence and K / V
+// head, m = row G + head: one read of a K / V tile serves all G query heads. Scores
+// are computed transposed, S^T = K Q^T (v_mfma_f32_32x32x16), so a lane holds 16
+// keys of one row: the softmax needs one exchange between the two lane halves, and
+// its numerators, as they lie, are the right operand of O^T = V^T P^T (the sum over
+// keys may be taken in any order, so the keys of a step are those a lane has). V^T's
+// operand comes from the row-major V by the transposing LDS read.
+//
+// K / V tiles go global -> LDS without registers, double-buffered: the copies of tile
+// i + 1 are in flight while tile i is computed. 16-byte chunks of a row are stored
+// permuted by the row (`swz`), so that the reads of 32 rows and the transposing reads
+// of 4 rows touch different banks; the permutation is in the copy's global address.
+//
+// Split of the work. A workgroup has 4 wavefronts, WM along the rows (32 each) and
+// WK = 4 / WM along the keys: few rows take WM = 1, where the wavefronts walk
+// different key tiles without a barrier and join at the end. Where the tiles alone
+// would leave compute units idle, the keys are also split over workgroups and a
+// second kernel joins the parts.
 #include "paged.h"
 
 namespace {
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+#define LDS_PTR(T, addr) ((__attribute__((address_space(3))) T*)(uint32_t)(addr))
+
+template <typename T>
+struct Num;
+template <>
+struct Num<__bf16> {
+  typedef bf16x8 vec8;
+  // numerators reach 2^(x - r) <= 2^LIM; a new reference is the maximum - SHIFT
+  static constexpr float SHIFT = 0.f, LIM = 8.f;
+  static constexpr uint16_t MAX = 0x7f7f;  // bits of the largest finite value
+  static __device__ __forceinline__ f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Num<_Float16> {
+  typedef f16x8 vec8;
+  static constexpr float SHIFT = 8.f, LIM = 14.f;
+  static constexpr uint16_t MAX = 0x7bff;
+  static __device__ __forceinline__ f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+
+// A launch covers the sequences with m_lo < rows x G <= m_hi.
+struct AttnLaunch {
+  int64_t m_lo, m_hi;
+  int slots;   // row tiles' places: tile t of sequence s at floor(q_start[s] G / BM) + s + t
+  int splits;  // key splits of `chunk` keys
+  int chunk;
+  float* ws;   // splits > 1: [slots][Hkv][splits] x ([BM][D] sums, [BM][2] reference and l)
+};
+
+template <int WM>
+struct Shape {
+  static constexpr int WK = 4 / WM, BM = 32 * WM;
+  static constexpr int KT = WM == 1 ? 32 : 64;  // keys of a tile
+};
+
+template <int D>
+constexpr int part_floats(int bm) { return bm * (D + 2); }
+
+// position limit: keys at or past it are hidden from a row at position p
+__device__ __forceinline__ int key_limit(int p, int block, int len) {
+  if (block == 0) return len;
+  if (p < 0) return 0;
+  const int64_t lim = ((int64_t)(p / block) + 1) * block;
+  return lim < len ? (int)lim : len;
+}
+
+__device__ __forceinline__ float max_halves(float v) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float sum_halves(float v) {
+  const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(p[0]) + __uint_as_float(p[1]);
+}
+
+struct Seq {
+  int start, n, len;
+};
+// false: no such sequence, or one outside the call's bounds
+__device__ __forceinline__ bool read_seq(const PagedAttnArgs& a, int s, Seq& q) {
+  if (s < 0 || s >= a.batch.n_seq) return false;
+  const int start = a.batch.q_start[s], end = a.batch.q_start[s + 1];
+  q = {start, end - start, a.batch.kv_len[s]};
+  return start >= 0 && end > start && end <= a.batch.rows && q.n <= a.max_rows && q.len >= 0 &&
+         q.len <= a.max_len;
+}
+
+// nonzero for each of the two 16-bit values that is infinite or NaN
+template <typename T>
+__device__ __forceinline__ u16x2 over_finite(uint32_t v) {
+  return __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, v & 0x7fff7fffu),
+                                       u16x2{Num<T>::MAX, Num<T>::MAX});
+}
+
+// chunk permutation of a K / V row in LDS (D / 8 chunks of 16 bytes)
+template <int D>
+__device__ __forceinline__ int swz(int row) {
+  if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+  return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+template <typename T, int D, int WM, bool CAP>
+__global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArgs a, AttnLaunch L) {
+  typedef Num<T> N;
+  typedef typename N::vec8 vec8;
+  constexpr int WK = Shape<WM>::WK, BM = Shape<WM>::BM, KT = Shape<WM>::KT, NB = KT / 32;
+  constexpr int TILE = KT * D * 2, STAGE = 2 * TILE;     // bytes of K or V, of both
+  constexpr int GROUPS = KT / 16, MYG = WM == 4 ? 1 : 2; // 16-row groups of a tile, a wavefront's
+  constexpr int RPI = 512 / D, IPG = 16 / RPI;           // rows of a copy, copies of a group
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave % WM, wk = wave / WM;
+  const int Hkv = a.pages.kv_heads, G = a.heads / Hkv, ps = a.pages.page_size;
+  const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv;
+  const int split = rest % L.splits, slot = L.slots - 1 - rest / L.splits;
+
+  // which sequence and row tile
+  int s, tile = 0;
+  if constexpr (WM == 1) {
+    s = slot;
+  } else {
+    int n = 0;
+    for (int base = 0; base < a.batch.n_seq; base += 64) {
+      const int i = base + lane;
+      const bool at = i < a.batch.n_seq && (int64_t)a.batch.q_start[i] * G / BM + i <= slot;
+      n += __popcll(__ballot(at));
+    }
+    s = __builtin_amdgcn_readfirstlane(n) - 1;
+  }
+  Seq q;
+  if (!read_seq(a, s, q)) return;
+  if constexpr (WM != 1) tile = slot - (int)((int64_t)q.start * G / BM + s);
+  const int64_t M = (int64_t)q.n * G;
+  if (M <= L.m_lo || M > L.m_hi || (int64_t)tile * BM >= M) return;
+  const int m0 = tile * BM, m1 = (int)(M < m0 + BM ? M : m0 + BM);  // this tile's rows
+  const int pos0 = q.len - q.n;
+  const int lim_tile = key_limit(pos0 + (m1 - 1) / G, a.block, q.len);
+  const int k0 = split * L.chunk;
+  if (split > 0 && k0 >= lim_tile) return;
+  const int k1 = lim_tile < k0 + L.chunk ? lim_tile : k0 + L.chunk;
+
+  // this lane's row (a row tile's last rows repeat its last one and are not stored)
+  const int c = lane & 31, h = lane >> 5;
+  const int w0 = m0 + 32 * wm;  // the wavefront's first row
+  const int m = w0 + c < m1 ? w0 + c : m1 - 1;
+  const int row = q.start + m / G, head = kvh * G + m % G;
+  const int lim = key_limit(pos0 + m / G, a.block, q.len);
+  const bool idle = w0 >= m1;
+  const int lim_min = idle ? 0 : key_limit(pos0 + w0 / G, a.block, q.len);
+  const int lim_max = idle ? 0 : key_limit(pos0 + ((w0 + 31 < m1 ? w0 + 31 : m1 - 1)) / G, a.block, q.len);
+
+  vec8 qf[D / 16];
+  {
+    const T* qp = (const T*)a.q + row * a.ld_q + head * D + 8 * h;
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) qf[st] = *(const vec8*)(qp + 16 * st);
+    if (a.scale < 0.f)
+#pragma unroll
+      for (int st = 0; st < D / 16; ++st) qf[st] = -qf[st];
+  }
+  const float sc = fabsf(a.scale) * 1.44269504f;
+
+  // copies: this lane's offset inside a 16-row group
+  uint32_t voff[IPG];
+#pragma unroll
+  for (int i = 0; i < IPG; ++i) {
+    const int r = RPI * i + lane / (D / 8);
+    voff[i] = r * D * 2 + (((lane % (D / 8)) ^ swz<D>(r)) << 4);
+  }
+  const uint32_t ring = lds0 + wk * 2 * STAGE;
+  const int64_t page_elems = (int64_t)Hkv * ps * D;
+  const T* const kbase = (const T*)a.pages.k + (int64_t)kvh * ps * D;
+  const T* const vbase = (const T*)a.pages.v + (int64_t)kvh * ps * D;
+  const int32_t* const table = a.batch.table + (int64_t)s * a.batch.table_ld;
+
+  // the pages of a tile: lane j < GROUPS reads that of 16-key group j (-1: none there)
+  const int first = k0 / KT + wk, last = (k1 + KT - 1) / KT;  // key tiles first, first + WK, ... < last
+  const int iters = (last - k0 / KT + WK - 1) / WK;
+  auto page_of = [&](int t) {
+    const int p = t * KT + 16 * (lane % GROUPS);
+    return p < k1 ? table[p / ps] : -1;
+  };
+  auto issue = [&](int t, int ids, int buf) {
+#pragma unroll
+    for (int g = 0; g < MYG; ++g) {
+      const int j = WM == 1 ? g : WM == 2 ? 2 * wm + g : wm;
+      const int id = __builtin_amdgcn_readlane(ids, j);
+      const bool ok = id >= 0 && id < a.pages.n_pages;
+      const int64_t off = ok ? id * page_elems + (int64_t)((t * KT + 16 * j) % ps) * D : 0;
+      const uint32_t to = ring + buf * STAGE + j * 16 * D * 2;
+#pragma unroll
+      for (int i = 0; i < IPG; ++i) copy_to_lds(kbase + off, voff[i], to + i * 1024);
+#pragma unroll
+      for (int i = 0; i < IPG; ++i) copy_to_lds(vbase + off, voff[i], to + TILE + i * 1024);
+    }
+  };
+  auto there = [&](int ids) {  // bit j: group j has a page
+    return (uint32_t)(__ballot(ids >= 0 && ids < a.pages.n_pages) & ((1u << GROUPS) - 1));
+  };
+
+  f32x16 o[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  float ref = -INFINITY, l = 0.f;
+  bool put_back = false;
+
+  // LDS addresses inside a stage: K rows by chunk step, V by (dimension block, key half)
+  const uint32_t k_row = c * D * 2, k_swz = (h ^ swz<D>(c)) << 4;
+  const int v_r = 4 * h + ((lane & 15) >> 2);
+  const uint32_t v_row = TILE + v_r * D * 2 + 8 * (lane & 1);
+  const uint32_t v_swz = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz<D>(v_r)) << 4;
+  auto read_v = [&](uint32_t base, int t, int db) {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        LDS_PTR(s16x4, base + v_row + (v_swz ^ (db << 6)) + t * 16 * D * 2));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        LDS_PTR(s16x4, base + v_row + (v_swz ^ (db << 6) ^ 32) + (t * 16 + 8) * D * 2));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(vec8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  int ids = iters > 0 ? page_of(first) : -1;
+  uint32_t have = there(ids);
+  if (iters > 0) issue(first, ids, 0);
+  ids = iters > 1 ? page_of(first + WK) : -1;
+  for (int it = 0; it < iters; ++it) {
+    const int t = first + it * WK;
+    wait_loads();
+    if constexpr (WM > 1)
+      lds_barrier();  // every wavefront's copies of tile it have landed, tile it - 1 is done with
+    else
+      wait_lds();
+    uint32_t have_next = 0;
+    if (it + 1 < iters) {
+      have_next = there(ids);
+      issue(t + WK, ids, (it + 1) & 1);
+      ids = it + 2 < iters ? page_of(t + 2 * WK) : -1;
+    }
+    const int kt = t * KT;
+    if (kt < lim_max) {
+      const uint32_t base = ring + (it & 1) * STAGE;
+      f32x16 x[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[nb][i] = 0.f;
+#pragma unroll
+      for (int st = 0; st < D / 16; ++st)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const u32x4 kf = *LDS_PTR(u32x4, base + k_row + (k_swz ^ (st << 5)) + nb * 32 * D * 2);
+          x[nb] = N::mfma(__builtin_bit_cast(vec8, kf), qf[st], x[nb]);
+        }
+      if constexpr (CAP) {
+        // log2(e) cap tanh(s / cap), tanh(y) = 1 - 2 / (e^(2y) + 1); a NaN stays one
+        const float in = 2.f * sc / a.softcap, out = 1.44269504f * a.softcap;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            x[nb][i] = out - 2.f * out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[nb][i] * in) + 1.f);
+      } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[nb][i] *= sc;
+      }
+      const bool clean = have == (1u << GROUPS) - 1 && kt + KT <= lim_min;
+      if (!clean) {
+        // hidden keys: those at or past the row's limit and those of missing pages
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int grp = nb * 2 + i / 8;
+            const int end = (have >> grp) & 1 ? lim - kt - 4 * h : INT32_MIN;
+            if (nb * 32 + 8 * (i / 4) + i % 4 >= end) x[nb][i] = -INFINITY;
+          }
+      }
+      float mt = x[0][0];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, x[nb][i]);
+      mt = max_halves(mt);
+      if (__any(mt > ref + N::LIM)) {
+        const float next = mt > ref + N::LIM ? mt - N::SHIFT : ref;
+        const float f = ref == next ? 1.f : __builtin_amdgcn_exp2f(ref - next);
+        l *= f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= f;
+        ref = next;
+      }
+      const float r = ref == -INFINITY ? 0.f : ref;  // no key seen so far
+      vec8 pf[2 * NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float p = __builtin_amdgcn_exp2f(x[nb][i] - r);
+          l += p;
+          pf[2 * nb + i / 8][i % 8] = (T)p;
+        }
+      // A value of V that is not finite would reach the rows that do not see its key as
+      // 0 x infinity. Where a tile hides keys from some row such values are taken as zeros
+      // here and put back after the loop for the rows that see them.
+      bool odd = false;
+      if (!clean) {
+        u16x2 any = {};
+#pragma nounroll
+        for (int tt = 0; tt < 2 * NB; ++tt)
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) {
+            const u32x4 v = __builtin_bit_cast(u32x4, read_v(base, tt, db));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) any |= over_finite<T>(v[j]);
+          }
+        odd = __any(__builtin_bit_cast(uint32_t, any) != 0);
+      }
+      if (!odd) {
+#pragma unroll
+        for (int tt = 0; tt < 2 * NB; ++tt)
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) o[db] = N::mfma(read_v(base, tt, db), pf[tt], o[db]);
+      } else {
+        put_back = true;
+#pragma nounroll
+        for (int tt = 0; tt < 2 * NB; ++tt) {
+          vec8 p = pf[0];
+#pragma unroll
+          for (int k = 1; k < 2 * NB; ++k)
+            if (k == tt) p = pf[k];
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db) {
+            u32x4 v = __builtin_bit_cast(u32x4, read_v(base, tt, db));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const u16x2 d = over_finite<T>(v[j]);
+              if (d[0]) v[j] &= 0xffff0000u;
+              if (d[1]) v[j] &= 0xffffu;
+            }
+            o[db] = N::mfma(__builtin_bit_cast(vec8, v), p, o[db]);
+          }
+        }
+      }
+    }
+    have = have_next;
+  }
+  l = sum_halves(l);
+  if (put_back) {
+    // the wavefront's tiles in which some row has hidden keys: infinities and NaN of V, to
+    // the rows that see them
+    for (int it = 0; it < iters; ++it) {
+      const int kt = (first + it * WK) * KT;
+      for (int p = kt; p < kt + KT && p < lim_max && p < k1; ++p) {
+        const int id = table[p / ps];
+        if (id < 0 || id >= a.pages.n_pages) continue;
+        if (kt + KT <= lim_min && there(page_of(first + it * WK)) == (1u << GROUPS) - 1) break;
+        const T* v = vbase + id * page_elems + (int64_t)(p % ps) * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float y = (float)v[32 * db + 8 * (i / 4) + i % 4];
+            if (p < lim && !(fabsf(y) < INFINITY)) o[db][i] += y;
+          }
+      }
+    }
+  }
+
+  float* part = nullptr;
+  const bool whole = lim_tile <= L.chunk;  // no other workgroup has keys of this tile
+  if (!whole)
+    part = L.ws + (((int64_t)slot * Hkv + kvh) * L.splits + split) * part_floats<D>(BM);
+  T* const out = (T*)a.out;
+  const float ln2 = 0.69314718f;
+
+  if constexpr (WK == 1) {
+    if (w0 + c < m1) {
+      if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T* op = out + row * a.ld_out + head * D + 4 * h;
+        typedef T vec4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            vec4 w;
+            for (int e = 0; e < 4; ++e) w[e] = (T)(l == 0.f ? 0.f : o[db][4 * i + e] * inv);
+            *(vec4*)(op + 32 * db + 8 * i) = w;
+          }
+        if (a.lse && h == 0)
+          a.lse[(int64_t)row * a.heads + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * ln2;
+      } else {
+        float* pp = part + (32 * wm + c) * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f32x4 w;
+            for (int e = 0; e < 4; ++e) w[e] = o[db][4 * i + e];
+            *(f32x4*)(pp + 32 * db + 8 * i) = w;
+          }
+        if (h == 0) {
+          part[BM * D + 2 * (32 * wm + c)] = ref;
+          part[BM * D + 2 * (32 * wm + c) + 1] = l;
+        }
+      }
+    }
+  } else {
+    // join the key groups' sums through LDS
+    constexpr int LD = D + 4;
+    float* const so = (float*)smem;          // [WK][BM][LD]
+    float* const sr = so + WK * BM * LD;     // [WK][BM][2]
+    wait_loads();
+    __syncthreads();
+    {
+      float* p = so + (wk * BM + 32 * wm + c) * LD + 4 * h;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x4 w;
+          for (int e = 0; e < 4; ++e) w[e] = o[db][4 * i + e];
+          *(f32x4*)(p + 32 * db + 8 * i) = w;
+        }
+      if (h == 0) {
+        sr[(wk * BM + 32 * wm + c) * 2] = ref;
+        sr[(wk * BM + 32 * wm + c) * 2 + 1] = l;
+      }
+    }
+    __syncthreads();
+    constexpr int TPR = 256 / BM, E = D / TPR;  // threads of a row, values each
+    const int rr = threadIdx.x / TPR, e0 = (threadIdx.x % TPR) * E;
+    if (m0 + rr < m1) {
+      float top = -INFINITY, f[WK], sum = 0.f, acc[E];
+      for (int k = 0; k < WK; ++k) top = fmaxf(top, sr[(k * BM + rr) * 2]);
+      for (int e = 0; e < E; ++e) acc[e] = 0.f;
+      for (int k = 0; k < WK; ++k) {
+        const float rk = sr[(k * BM + rr) * 2];
+        f[k] = rk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rk - top);
+        // a part without keys has nothing to add (its l is 0, or NaN stays)
+        sum += f[k] == 0.f && rk == -INFINITY ? sr[(k * BM + rr) * 2 + 1] : f[k] * sr[(k * BM + rr) * 2 + 1];
+        for (int e = 0; e < E; e += 4) {
+          const f32x4 v = *(const f32x4*)(so + (k * BM + rr) * LD + e0 + e);
+          for (int u = 0; u < 4; ++u) acc[e + u] += rk == -INFINITY ? v[u] : f[k] * v[u];
+        }
+      }
+      const int mm = m0 + rr;
+      if (whole) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int64_t r2 = q.start + mm / G;
+        T* op = out + r2 * a.ld_out + (kvh * G + mm % G) * D + e0;
+        for (int e = 0; e < E; e += 8) {
+          vec8 w;
+          for (int u = 0; u < 8; ++u) w[u] = (T)(sum == 0.f ? 0.f : acc[e + u] * inv);
+          *(vec8*)(op + e) = w;
+        }
+        if (a.lse && e0 == 0)
+          a.lse[r2 * a.heads + kvh * G + mm % G] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * ln2;
+      } else {
+        for (int e = 0; e < E; e += 4)
+          *(f32x4*)(part + rr * D + e0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
+        if (e0 == 0) {
+          part[BM * D + 2 * rr] = top;
+          part[BM * D + 2 * rr + 1] = sum;
+        }
+      }
+    }
+  }
+}
+
+// Joins the parts of split rows: one wavefront per (row, query head).
 template <typename T, int D>
-__global__ void __launch_bounds__(64) paged_attention_kernel(PagedAttnArgs a) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x, head = blockIdx.x % a.heads, row = blockIdx.x / a.heads;
+__global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, AttnLaunch L, int bm) {
+  const int lane = threadIdx.x & 63;
+  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)(item / a.heads), head = (int)(item % a.heads);
+  if (row >= a.batch.rows) return;
   const int s = seq_of_row(a.batch.q_start, a.batch.n_seq, row);
-  if (s < 0) return;
-  const int start = a.batch.q_start[s], end = a.batch.q_start[s + 1], len = a.batch.kv_len[s];
-  if (start < 0 || row >= end || end > a.batch.rows || end - start > a.max_rows || len > a.max_len) return;
-  const int pos = len - (end - row), ps = a.pages.page_size, Hkv = a.pages.kv_heads;
-  int seen = len;
-  if (a.block > 0) {
-    const int64_t lim = pos < 0 ? 0 : ((int64_t)(pos / a.block) + 1) * a.block;
-    if (lim < seen) seen = (int)lim;
+  Seq q;
+  if (!read_seq(a, s, q) || row >= q.start + q.n) return;
+  const int Hkv = a.pages.kv_heads, G = a.heads / Hkv, kvh = head / G;
+  const int64_t M = (int64_t)q.n * G;
+  if (M <= L.m_lo || M > L.m_hi) return;
+  const int m = (row - q.start) * G + head % G, tile = m / bm, c = m % bm;
+  const int m1 = (int)(M < (tile + 1) * bm ? M : (tile + 1) * bm);
+  const int lim = key_limit(q.len - q.n + (m1 - 1) / G, a.block, q.len);
+  if (lim <= L.chunk) return;  // written by its only workgroup
+  const int parts = (lim + L.chunk - 1) / L.chunk;
+  const int slot = bm == 32 ? s : (int)((int64_t)q.start * G / bm + s) + tile;
+  const float* p0 = L.ws + ((int64_t)slot * Hkv + kvh) * L.splits * part_floats<D>(bm);
+  float top = -INFINITY;
+  for (int k = lane; k < parts; k += 64)
+    top = fmaxf(top, p0[(int64_t)k * part_floats<D>(bm) + bm * D + 2 * c]);
+  top = wave_max(top);
+  float sum = 0.f, acc[D / 64] = {};
+  for (int k = 0; k < parts; ++k) {
+    const float* p = p0 + (int64_t)k * part_floats<D>(bm);
+    const float r = p[bm * D + 2 * c], f = r == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r - top);
+    sum += f * p[bm * D + 2 * c + 1];
+    for (int e = 0; e < D / 64; ++e) acc[e] += f * p[c * D + lane * (D / 64) + e];
   }
-  const T* q = (const T*)a.q + row * a.ld_q + head * D;
-  float qv[E], o[E] = {};
-  for (int e = 0; e < E; ++e) qv[e] = (float)q[lane * E + e];
-  float m = -INFINITY, l = 0.f;
-  const int kvh = head / (a.heads / Hkv);
-  for (int p = 0; p < seen; ++p) {
-    const int page = a.batch.table[(int64_t)s * a.batch.table_ld + p / ps];
-    if (page < 0 || page >= a.pages.n_pages) continue;
-    const int64_t at = (((int64_t)page * Hkv + kvh) * ps + p % ps) * D + lane * E;
-    float x = 0.f;
-    for (int e = 0; e < E; ++e) x += qv[e] * (float)((const T*)a.pages.k)[at + e];
-    x = wave_sum(x) * a.scale;
-    if (a.softcap > 0.f) x = a.softcap * tanhf(x / a.softcap);
-    if (x == -INFINITY) continue;
-    const float m2 = fmaxf(m, x), f = expf(m - m2), w = expf(x - m2);
-    l = l * f + w;
-    for (int e = 0; e < E; ++e) o[e] = o[e] * f + w * (float)((const T*)a.pages.v)[at + e];
-    m = m2;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  T* op = (T*)a.out + row * a.ld_out + head * D + lane * (D / 64);
+  for (int e = 0; e < D / 64; ++e) op[e] = (T)(sum == 0.f ? 0.f : acc[e] * inv);
+  if (a.lse && lane == 0)
+    a.lse[(int64_t)row * a.heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// One launch's place in the plan: `tiles` row tiles are expected, `occ` workgroups fit a CU.
+PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, int64_t slots, int64_t tiles, int kv_heads, int d,
+                     int max_len) {
+  const int bm = 32 * wm, step = wm == 1 ? 4 * 32 : (4 / wm) * 64;
+  const int occ = (wm == 4 ? 2 : 1) * (d == 64 ? 2 : 1);
+  const int64_t want = 256 * occ, items = tiles * kv_heads;
+  int64_t splits = items > 0 ? want / items : 1;
+  const int64_t most = ceil_div(max_len, 2 * step);
+  splits = splits > most ? most : splits;
+  splits = splits < 1 ? 1 : splits;
+  const int64_t chunk = ceil_div(ceil_div(max_len, splits), step) * step;
+  splits = chunk > 0 ? ceil_div(max_len, chunk) : 1;
+  PagedPlan::Part p{};
+  p.wm = wm, p.m_lo = m_lo, p.m_hi = m_hi;
+  p.slots = slots, p.splits = (int)splits, p.chunk = (int)(chunk > 0 ? chunk : step);
+  p.ws_bytes = splits > 1 ? slots * kv_heads * splits * (int64_t)bm * (d + 2) * 4 : 0;
+  return p;
+}
+
+template <typename T, int D, int WM, bool CAP>
+hipError_t launch(const PagedAttnArgs& a, const AttnLaunch& L, hipStream_t s) {
+  constexpr int WK = Shape<WM>::WK, BM = Shape<WM>::BM, KT = Shape<WM>::KT;
+  constexpr int ring = WK * 2 * 2 * KT * D * 2;
+  constexpr int join = WK == 1 ? 0 : WK * BM * (D + 4 + 2) * 4;
+  constexpr int bytes = ring > join ? ring : join;
+  static_assert(bytes <= 160 * 1024, "LDS of one CU");
+  if constexpr (bytes > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)attn_kernel<T, D, WM, CAP>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
   }
-  T* out = (T*)a.out + row * a.ld_out + head * D;
-  for (int e = 0; e < E; ++e) out[lane * E + e] = (T)(l == 0.f ? 0.f : o[e] / l);
-  if (a.lse && lane == 0) a.lse[(int64_t)row * a.heads + head] = l == 0.f ? -INFINITY : m + logf(l);
+  const int64_t n = (int64_t)L.slots * L.splits * a.pages.kv_heads;
+  attn_kernel<T, D, WM, CAP><<<dim3((unsigned)n), dim3(256), bytes, s>>>(a, L);
+  return hipGetLastError();
 }
 
 template <typename T, int D>
-hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
-  // at most 2^24 rows and 1024 heads
-  const int64_t n = (int64_t)a.batch.rows * a.heads;
-  if (n >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-  paged_attention_kernel<T, D><<<dim3((unsigned)n), dim3(64), 0, s>>>(a);
-  return hipGetLastError();
+hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t s) {
+  char* ws = (char*)a.ws;
+  for (int i = 0; i < plan.n; ++i) {
+    const PagedPlan::Part& p = plan.part[i];
+    const AttnLaunch L{p.m_lo, p.m_hi, (int)p.slots, p.splits, p.chunk, (float*)ws};
+    ws += p.ws_bytes;
+    const bool cap = a.softcap > 0.f;
+    hipError_t e;
+    if (p.wm == 1)
+      e = cap ? launch<T, D, 1, true>(a, L, s) : launch<T, D, 1, false>(a, L, s);
+    else if (p.wm == 2)
+      e = cap ? launch<T, D, 2, true>(a, L, s) : launch<T, D, 2, false>(a, L, s);
+    else
+      e = cap ? launch<T, D, 4, true>(a, L, s) : launch<T, D, 4, false>(a, L, s);
+    if (e != hipSuccess) return e;
+    if (p.splits > 1) {
+      const int64_t n = ceil_div((int64_t)a.batch.rows * a.heads, 4);
+      attn_join_kernel<T, D><<<dim3((unsigned)n), dim3(256), 0, s>>>(a, L, 32 * p.wm);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
 }
 
 }  // namespace
 
-PagedPlan paged_attention_plan(int, int, int, int, int, int, int) { return {0}; }
+PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
+                               int max_len) {
+  PagedPlan plan{};
+  if (n_seq < 1 || rows < 1 || max_rows < 1) return plan;
+  if (max_rows > rows) max_rows = rows;
+  const int64_t G = heads / kv_heads, most = max_rows * G, all = INT64_MAX;
+  // rows of a sequence and K / V head: up to 32 (a decode step) the wavefronts split the
+  // keys, up to 64 half and half, above that they split the rows
+  const int wm = most <= 32 ? 1 : most <= 64 ? 2 : 4;
+  const bool even = rows == (int64_t)n_seq * max_rows;
+  const auto slots = [&](int bm) { return rows * G / bm + n_seq; };
+  if (wm == 1) {
+    plan.part[plan.n++] = part(1, 0, 32, n_seq, n_seq, kv_heads, d, max_len);
+  } else if (even) {
+    plan.part[plan.n++] = part(wm, 0, all, slots(32 * wm), n_seq * ceil_div(most, 32 * wm), kv_heads, d, max_len);
+  } else {
+    // unequal sequences: the short ones in a launch of their own
+    plan.part[plan.n++] = part(wm, 32, all, slots(32 * wm), ceil_div(rows * G, 32 * wm), kv_heads, d, max_len);
+    plan.part[plan.n++] = part(1, 0, 32, n_seq, n_seq, kv_heads, d, max_len);
+  }
+  for (int i = 0; i < plan.n; ++i) plan.bytes += plan.part[i].ws_bytes;
+  return plan;
+}
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan&, hipStream_t s) {
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
   const bool h = a.pages.dtype == LOPA_F16;
-  if (a.pages.head_dim == 64) return h ? launch<_Float16, 64>(a, s) : launch<__bf16, 64>(a, s);
-  return h ? launch<_Float16, 128>(a, s) : launch<__bf16, 128>(a, s);
+  if (a.pages.head_dim == 64) return h ? launch_all<_Float16, 64>(a, p, s) : launch_all<__bf16, 64>(a, p, s);
+  return h ? launch_all<_Float16, 128>(a, p, s) : launch_all<__bf16, 128>(a, p, s);
 }

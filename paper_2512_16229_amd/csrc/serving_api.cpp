@@ -43,6 +43,8 @@ int check_paged(const lopa_pages* p, const lopa_paged_batch* b, int32_t heads) {
   if (b->n_seq < 0 || b->n_seq > MAX_SEQ || b->rows < 0 || b->rows > MAX_BATCH_ROWS)
     return lopa_fail(LOPA_ESHAPE, "n_seq %d outside [0, %d] or rows %d outside [0, %d]", b->n_seq,
                      MAX_SEQ, b->rows, MAX_BATCH_ROWS);
+  if ((int64_t)b->rows * heads >= ((int64_t)1 << 31))
+    return lopa_fail(LOPA_ESHAPE, "%d rows of %d heads: need fewer than 2^31", b->rows, heads);
   if (b->n_seq && b->rows) {
     if (!b->table || !b->q_start || !b->kv_len)
       return lopa_fail(LOPA_EINVAL, "null table, q_start or kv_len");
@@ -67,10 +69,12 @@ int launched(hipError_t e, const char* what) {
   return e == hipSuccess ? LOPA_OK : lopa_fail(LOPA_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-int check_bounds(int32_t n_seq, int32_t rows, int32_t max_rows, int32_t max_len) {
+int check_bounds(int32_t heads, int32_t n_seq, int32_t rows, int32_t max_rows, int32_t max_len) {
   if (n_seq < 0 || n_seq > MAX_SEQ || rows < 0 || rows > MAX_BATCH_ROWS)
     return lopa_fail(LOPA_ESHAPE, "n_seq %d outside [0, %d] or rows %d outside [0, %d]", n_seq,
                      MAX_SEQ, rows, MAX_BATCH_ROWS);
+  if ((int64_t)rows * heads >= ((int64_t)1 << 31))
+    return lopa_fail(LOPA_ESHAPE, "%d rows of %d heads: need fewer than 2^31", rows, heads);
   if (max_rows < 0 || max_len < 0)
     return lopa_fail(LOPA_EINVAL, "max_rows %d or max_len %d negative", max_rows, max_len);
   if (max_len >= (1 << 30)) return lopa_fail(LOPA_ESHAPE, "max_len %d: need less than 2^30", max_len);
@@ -117,7 +121,7 @@ int64_t lopa_paged_attention_workspace(int32_t heads, int32_t kv_heads, int32_t 
                                        int32_t n_seq, int32_t rows, int32_t max_rows,
                                        int32_t max_len) {
   if (int e = check_heads(heads, kv_heads, head_dim)) return e;
-  if (int e = check_bounds(n_seq, rows, max_rows, max_len)) return e;
+  if (int e = check_bounds(heads, n_seq, rows, max_rows, max_len)) return e;
   return paged_attention_plan(heads, kv_heads, head_dim, n_seq, rows, max_rows, max_len).bytes;
 }
 
@@ -126,7 +130,7 @@ int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch,
                          int32_t block, float scale, float softcap, void* out, int64_t ld_out,
                          float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
   if (int e = check_paged(pages, batch, heads)) return e;
-  if (int e = check_bounds(batch->n_seq, batch->rows, max_rows, max_len)) return e;
+  if (int e = check_bounds(heads, batch->n_seq, batch->rows, max_rows, max_len)) return e;
   if (block < 0) return lopa_fail(LOPA_EINVAL, "block %d negative (0 full, 1 causal, c block-causal)", block);
   if (!std::isfinite(scale)) return lopa_fail(LOPA_EINVAL, "scale must be finite");
   if (!(softcap >= 0.f && std::isfinite(softcap)))
