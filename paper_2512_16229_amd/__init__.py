@@ -275,51 +275,77 @@ def lopa_window_commit(kv: KV, winner, win, stream=None):
 _DTYPES = {torch.bfloat16: LOPA_BF16, torch.float16: LOPA_F16, torch.float32: LOPA_F32}
 
 
-def _one_device(tensors: dict, stream):
-    """The device that holds every tensor (None: not given), and the stream there."""
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor):
-            raise TypeError(f"{name}: expected a torch tensor")
-        if t.device.type != "cuda":
-            raise ValueError(f"{name}: must be a device tensor")
-        if dev is not None and t.device != dev:
-            raise ValueError(f"{name}: on {t.device}, the others on {dev}")
-        dev = t.device
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    elif hasattr(stream, "device") and stream.device != dev:
-        raise ValueError(f"stream of {stream.device}, the tensors on {dev}")
-    return dev, _stream(stream)
+def _on(t, name):
+    """The device of a call: that of its first tensor."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: must be a device tensor")
+    return t.device
 
 
-def _rows(t, shape, dtype, name):
-    """[rows][heads][head_dim] with contiguous heads: its pointer and row stride."""
-    if tuple(t.shape) != shape:
+def _arg(t, dtype, dev, name, shape=None):
+    """Address of a contiguous tensor on dev, None for None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.device != dev:
+        raise ValueError(f"{name}: must be a device tensor on {dev}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_arg(t, dtype, dev, name, shape):
+    """Address and row stride of a [rows][heads][head_dim] tensor with contiguous heads."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor")
+    if t.device != dev:
+        raise ValueError(f"{name}: must be a device tensor on {dev}")
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
     n, h, d = shape
-    if t.numel() and (t.stride(2) != 1 or (h > 1 and t.stride(1) != d)):
+    ld, sh, sd = t.stride()
+    if n and (sd != 1 or (h > 1 and sh != d)):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
-    return C.c_void_p(t.data_ptr()), t.stride(0) if n > 1 else h * d
+    return t.data_ptr(), ld if n > 1 else h * d
 
 
-def _paged(k_pages, v_pages, table, q_start, kv_len, rows):
-    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape:
-        raise ValueError("k_pages, v_pages: expected one shape [pages][kv_heads][page_size][head_dim]")
-    if k_pages.dtype not in (torch.bfloat16, torch.float16):
-        raise TypeError(f"k_pages: expected bfloat16 or float16, got {k_pages.dtype}")
-    n_seq = kv_len.numel()
-    if table.dim() != 2 or table.shape[0] != n_seq or q_start.numel() != n_seq + 1:
-        raise ValueError("table, q_start, kv_len: expected [n_seq][pages], [n_seq + 1] and [n_seq]")
+def _call(f, dev, stream, *args):
+    """f(*args, stream) on the device that holds the arrays, on its current stream or the given one."""
+    if stream is None:
+        st = torch.cuda.current_stream(dev).cuda_stream
+    else:
+        if hasattr(stream, "device") and stream.device != dev:
+            raise ValueError(f"stream of {stream.device}, the tensors on {dev}")
+        st = _stream(stream)
+    if torch.cuda.current_device() == dev.index:
+        _check(f(*args, st))
+    else:
+        with torch.cuda.device(dev):
+            _check(f(*args, st))
+
+
+def _paged(k_pages, v_pages, table, q_start, kv_len, rows, dev):
+    dtype = k_pages.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        raise TypeError(f"k_pages: expected bfloat16 or float16, got {dtype}")
+    if k_pages.dim() != 4:
+        raise ValueError("k_pages: expected [pages][kv_heads][page_size][head_dim]")
     n, hkv, ps, d = k_pages.shape
-    pages = lopa_pages(_ptr(k_pages, k_pages.dtype, "k_pages"), _ptr(v_pages, k_pages.dtype, "v_pages"),
-                       n, hkv, ps, d, _DTYPES[k_pages.dtype])
-    batch = lopa_paged_batch(_ptr(table, I32, "table"), _ptr(q_start, I32, "q_start"),
-                             _ptr(kv_len, I32, "kv_len"), n_seq, table.shape[1], rows)
+    n_seq, ld = table.shape if table.dim() == 2 else (-1, 0)
+    pages = lopa_pages(_arg(k_pages, dtype, dev, "k_pages"),
+                       _arg(v_pages, dtype, dev, "v_pages", k_pages.shape), n, hkv, ps, d, _DTYPES[dtype])
+    batch = lopa_paged_batch(_arg(table, I32, dev, "table", (n_seq, ld)),
+                             _arg(q_start, I32, dev, "q_start", (n_seq + 1,)),
+                             _arg(kv_len, I32, dev, "kv_len", (n_seq,)), n_seq, ld, rows)
     return pages, batch
 
 
@@ -327,25 +353,19 @@ def lopa_paged_append(k_pages, v_pages, table, q_start, kv_len, q, k, v, q_norm,
                       rope_theta, q_out, stream=None):
     """q [rows][heads][d], k and v [rows][kv_heads][d] (row strides are free, so views of a
     packed projection output do); q_norm / k_norm [d] or None; q_out like q."""
-    dev, st = _one_device(dict(k_pages=k_pages, v_pages=v_pages, table=table, q_start=q_start,
-                               kv_len=kv_len, q=q, k=k, v=v, q_norm=q_norm, k_norm=k_norm,
-                               q_out=q_out), stream)
-    if q.dim() != 3:
-        raise ValueError("q: expected [rows][heads][head_dim]")
-    rows, heads = q.shape[:2]
-    pages, batch = _paged(k_pages, v_pages, table, q_start, kv_len, rows)
-    t, hkv, d = k_pages.dtype, k_pages.shape[1], k_pages.shape[3]
-    for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
-        if w is not None and tuple(w.shape) != (d,):
-            raise ValueError(f"{name}: expected shape {(d,)}, got {tuple(w.shape)}")
-    qp, ldq = _rows(q, (rows, heads, d), t, "q")
-    kp, ldk = _rows(k, (rows, hkv, d), t, "k")
-    vp, ldv = _rows(v, (rows, hkv, d), t, "v")
-    op, ldo = _rows(q_out, (rows, heads, d), t, "q_out")
-    with torch.cuda.device(dev):
-        _check(lib.lopa_paged_append(C.byref(pages), C.byref(batch), heads, qp, ldq, kp, ldk, vp, ldv,
-                                     _ptr(q_norm, t, "q_norm"), _ptr(k_norm, t, "k_norm"), float(eps),
-                                     float(rope_theta), op, ldo, st))
+    dev = _on(k_pages, "k_pages")
+    rows, heads, d = q.shape
+    pages, batch = _paged(k_pages, v_pages, table, q_start, kv_len, rows, dev)
+    t, hkv = k_pages.dtype, pages.kv_heads
+    if d != pages.head_dim:
+        raise ValueError(f"q: head_dim {d}, the pages' {pages.head_dim}")
+    qp, ldq = _rows_arg(q, t, dev, "q", (rows, heads, d))
+    kp, ldk = _rows_arg(k, t, dev, "k", (rows, hkv, d))
+    vp, ldv = _rows_arg(v, t, dev, "v", (rows, hkv, d))
+    op, ldo = _rows_arg(q_out, t, dev, "q_out", (rows, heads, d))
+    _call(lib.lopa_paged_append, dev, stream, C.byref(pages), C.byref(batch), heads, qp, ldq, kp, ldk, vp,
+          ldv, _arg(q_norm, t, dev, "q_norm", (d,)), _arg(k_norm, t, dev, "k_norm", (d,)), eps, rope_theta,
+          op, ldo)
 
 
 def lopa_paged_attention_workspace(heads, kv_heads, head_dim, n_seq, rows, max_rows, max_len) -> int:
@@ -361,23 +381,17 @@ def lopa_paged_attention(q, k_pages, v_pages, table, q_start, kv_len, max_rows, 
     """q and out [rows][heads][d] (free row strides); block 0 full, 1 causal, c block-causal;
     lse [rows][heads] fp32 or None; workspace: a contiguous tensor of the bytes that
     lopa_paged_attention_workspace gives, or None."""
-    dev, st = _one_device(dict(q=q, k_pages=k_pages, v_pages=v_pages, table=table, q_start=q_start,
-                               kv_len=kv_len, out=out, lse=lse, workspace=workspace), stream)
-    if q.dim() != 3:
-        raise ValueError("q: expected [rows][heads][head_dim]")
-    rows, heads = q.shape[:2]
-    pages, batch = _paged(k_pages, v_pages, table, q_start, kv_len, rows)
-    t, d = k_pages.dtype, k_pages.shape[3]
-    qp, ldq = _rows(q, (rows, heads, d), t, "q")
-    op, ldo = _rows(out, (rows, heads, d), t, "out")
-    if lse is not None and tuple(lse.shape) != (rows, heads):
-        raise ValueError(f"lse: expected shape {(rows, heads)}, got {tuple(lse.shape)}")
-    size = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    with torch.cuda.device(dev):
-        _check(lib.lopa_paged_attention(C.byref(pages), C.byref(batch), heads, max_rows, max_len, qp, ldq,
-                                        block, float(scale), float(softcap), op, ldo,
-                                        _ptr(lse, F32, "lse"), _ptr(workspace, None, "workspace"), size,
-                                        st))
+    dev = _on(k_pages, "k_pages")
+    rows, heads, d = q.shape
+    pages, batch = _paged(k_pages, v_pages, table, q_start, kv_len, rows, dev)
+    if d != pages.head_dim:
+        raise ValueError(f"q: head_dim {d}, the pages' {pages.head_dim}")
+    t = k_pages.dtype
+    qp, ldq = _rows_arg(q, t, dev, "q", (rows, heads, d))
+    op, ldo = _rows_arg(out, t, dev, "out", (rows, heads, d))
+    _call(lib.lopa_paged_attention, dev, stream, C.byref(pages), C.byref(batch), heads, max_rows, max_len,
+          qp, ldq, block, scale, softcap, op, ldo, _arg(lse, F32, dev, "lse", (rows, heads)),
+          _arg(workspace, None, dev, "workspace"), workspace.nbytes if workspace is not None else 0)
 
 
 def lopa_token_logprobs_workspace(rows, vocab, n_top) -> int:
@@ -393,29 +407,22 @@ def lopa_token_logprobs(logits, tokens, exclude, logprob=None, entropy=None, top
     """logits [rows][vocab] of bfloat16, float16 or float32 (free row stride); tokens [rows] with
     logprob [rows]; entropy [rows]; top_ids and top_logprobs [rows][n]; each output may be None.
     exclude: a token outside the support, or -1."""
-    dev, st = _one_device(dict(logits=logits, tokens=tokens, logprob=logprob, entropy=entropy,
-                               top_ids=top_ids, top_logprobs=top_logprobs, workspace=workspace), stream)
-    if logits.dim() != 2 or logits.dtype not in _DTYPES:
+    dev = _on(logits, "logits")
+    dtype = _DTYPES.get(logits.dtype)
+    if dtype is None or logits.dim() != 2:
         raise TypeError("logits: expected [rows][vocab] of bfloat16, float16 or float32")
     rows, vocab = logits.shape
-    if logits.numel() and logits.stride(1) != 1:
+    ld, unit = logits.stride()
+    if rows and vocab > 1 and unit != 1:
         raise ValueError("logits: a row must be contiguous")
     n = top_ids.shape[-1] if top_ids is not None else 0
-    for name, t, shape in (("tokens", tokens, (rows,)), ("logprob", logprob, (rows,)),
-                           ("entropy", entropy, (rows,)), ("top_ids", top_ids, (rows, n)),
-                           ("top_logprobs", top_logprobs, (rows, n))):
-        if t is not None and tuple(t.shape) != shape:
-            raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
     if n == 0:
         top_ids = top_logprobs = None
-    size = workspace.numel() * workspace.element_size() if workspace is not None else 0
-    with torch.cuda.device(dev):
-        _check(lib.lopa_token_logprobs(C.c_void_p(logits.data_ptr()), _DTYPES[logits.dtype],
-                                       logits.stride(0) if rows > 1 else vocab, rows, vocab, exclude,
-                                       _ptr(tokens, I32, "tokens"), n, _ptr(logprob, F32, "logprob"),
-                                       _ptr(entropy, F32, "entropy"), _ptr(top_ids, I32, "top_ids"),
-                                       _ptr(top_logprobs, F32, "top_logprobs"),
-                                       _ptr(workspace, None, "workspace"), size, st))
+    _call(lib.lopa_token_logprobs, dev, stream, logits.data_ptr(), dtype, ld if rows > 1 else vocab, rows,
+          vocab, exclude, _arg(tokens, I32, dev, "tokens", (rows,)), n,
+          _arg(logprob, F32, dev, "logprob", (rows,)), _arg(entropy, F32, dev, "entropy", (rows,)),
+          _arg(top_ids, I32, dev, "top_ids", (rows, n)), _arg(top_logprobs, F32, dev, "top_logprobs", (rows, n)),
+          _arg(workspace, None, dev, "workspace"), workspace.nbytes if workspace is not None else 0)
 
 
 from .decoder import Decoder, WindowDecoder  # noqa: E402,F401

@@ -239,7 +239,8 @@ hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hi
 
 // ------------------------------------------- serving: log probabilities
 struct LogprobPlan {
-  int64_t bytes;  // workspace
+  int64_t bytes;       // workspace
+  int64_t workgroups;  // of the largest launch
 };
 LogprobPlan logprobs_plan(int rows, int vocab, int n_top);
 struct LogprobArgs {
