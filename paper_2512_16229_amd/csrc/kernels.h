@@ -238,11 +238,7 @@ struct PagedAttnArgs {
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s);
 
 // ------------------------------------------- serving: log probabilities
-struct LogprobPlan {
-  int64_t bytes;       // workspace
-  int64_t workgroups;  // of the largest launch
-};
-LogprobPlan logprobs_plan(int rows, int vocab, int n_top);
+int64_t logprobs_workspace(int rows, int vocab, int n_top);  // bytes
 struct LogprobArgs {
   const void* logits;
   int dtype;
@@ -255,4 +251,4 @@ struct LogprobArgs {
   float* top_logprobs;
   void* ws;
 };
-hipError_t launch_token_logprobs(const LogprobArgs& a, const LogprobPlan& p, hipStream_t s);
+hipError_t launch_token_logprobs(const LogprobArgs& a, hipStream_t s);

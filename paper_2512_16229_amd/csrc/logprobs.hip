@@ -1,29 +1,43 @@
 // Log probabilities of given tokens, entropy and the most probable tokens of rows
 // of logits.
 //
-// Mathematics. With a reference m (the largest logit), S = sum 2^((x - m) log2 e) and
-// T = sum (x - m) 2^(...): ln p_t = (x_t - m) - ln S, entropy = ln S - T / S; two
-// pieces join as (S 2^d + S', (T + (m - m') S) 2^d + T') with d = (m - m') log2 e.
+// Mathematics. In units of log2: with y = x log2 e and a reference r (of the largest
+// logit), S = sum 2^(y - r) and T = sum (y - r) 2^(y - r): ln p_t = (y_t - r - log2 S) ln 2,
+// entropy = (log2 S - T / S) ln 2; a piece moves to another reference by 2^(r - r') and
+// T + (r - r') S.
 //
-// What bounds it: memory, every logit read once (16-bit rows near the vector units
-// too: six operations a logit, one of them an exponential at a quarter of the rate).
-// A workgroup takes a segment of a row, THREADS x NV 16-byte vectors, into registers
-// and makes everything of it there; a second kernel joins the segments of a row.
+// What bounds it: memory, every logit read once (16-bit rows near the vector units too:
+// nine operations a logit counting the exponential as four).
+// A workgroup streams a part of a row, segments of THREADS x NV 16-byte vectors, the
+// next one's loads in flight while one is summed; every thread keeps its own r, S and T,
+// so nothing is exchanged before the end. A second kernel joins the parts of a row.
 //
-// Top tokens. The n-th largest maximum of groups of lanes is a bound that at least n
-// logits of the segment reach (each wavefront's, then the largest of the four); with
-// twice as many groups as n about 1.4 n logits pass it. Those go to LDS as 64-bit keys
-// that order by (value, lowest token), and a key's rank is the number of larger ones.
-// Rows of many equal values can pass more than CAND; they are taken one by one.
+// Top tokens. The pass only keeps the maximum of every group of 16 vectors (256 bytes,
+// consecutive tokens). The n best groups by (maximum, lowest group) hold the n best
+// tokens by (value, lowest token): a token of another group is behind the best token of
+// each of the n. They are found among the maxima, and their logits are read again and
+// ranked. (Keeping the n best of each wavefront's stream in the pass itself took 48
+// instead of 30 us at 256 rows of 152064 fp32 logits, n = 20: nearly every segment
+// brings some logit that passes.)
+// Selection works on 64-bit keys that order by (value, lowest index). A wavefront's
+// bound is the n-th largest maximum of groups of lanes (with twice as many groups as n
+// about 1.4 n keys pass it); what passes goes to a buffer in LDS, and a full one is cut
+// to the n best, a key's rank being the number of larger ones.
 #include "common.h"
 #include "kernels.h"
+
+#include <type_traits>
 
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int CAND = 1024;
-constexpr int LISTS = 64;  // segments that a join takes at a time, the result so far among them
-constexpr float LOG2E = 1.44269504f;
+constexpr int CAND = 192;    // keys of a wavefront's buffer: room for 64 more while it holds up to 128
+constexpr int STEP = 8;      // keys read at a time, the last ones padded with 0
+constexpr int GROUP = 16;    // vectors of a group
+constexpr int LDS_GROUPS = 4096;  // groups of a row whose maxima stay in LDS where one workgroup has the row
+constexpr int PARTS = 256;   // parts of a row at most
+constexpr float LOG2E = 1.44269504f, LN2 = 0.69314718f;
+constexpr float HUGE_X = 1e30f;  // references past it: y overflows, and equal logits are 0 apart, others infinitely
 typedef unsigned long long u64;
 
 // order of (value, token): larger value first, then lower token; 0: nothing
@@ -38,224 +52,352 @@ __device__ __forceinline__ float value_of(u64 k) {
   return __uint_as_float((b & 0x80000000u) ? b & 0x7fffffffu : ~b);
 }
 
+// y - r for a logit x and the logit m of the reference; the reference is m log2 e as rounded
+__device__ __forceinline__ float above(float x, float m) {
+  return fabsf(m) < HUGE_X ? fmaf(x, LOG2E, -(m * LOG2E)) : (x - m) * LOG2E;
+}
+// the same between two references (the products rounded first, as references are: a fused
+// one leaves its rounding error, which is large for large logits)
+__device__ __forceinline__ float between(float m, float to) {
+#pragma clang fp contract(off)
+  return fabsf(m) < HUGE_X && fabsf(to) < HUGE_X ? m * LOG2E - to * LOG2E : (m - to) * LOG2E;
+}
+
 struct Sums {
   float m, S, T;
 };
-// a NaN in S stays (a row with a NaN or +inf has no distribution)
-__device__ __forceinline__ Sums join(Sums a, Sums b) {
-  const float m = fmaxf(a.m, b.m);
+// s at the reference of the logit m >= s.m (a NaN stays: a row with a NaN or +inf has no
+// distribution)
+__device__ __forceinline__ Sums moved(Sums s, float m) {
+  if (s.m == -INFINITY) return {m, s.S, 0.f};
+  const float d = between(s.m, m), f = __builtin_amdgcn_exp2f(d);
+  return {m, s.S * f, (s.T + fmaxf(d, -300.f) * s.S) * f};
+}
+// the workgroup's sums: every thread gets them
+__device__ __forceinline__ Sums block_sums(Sums s, float* lds) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float mw = wave_max(s.m);
+  s = moved(s, mw);
+  s.S = wave_sum(s.S), s.T = wave_sum(s.T);
+  if (lane == 0) lds[3 * wave] = mw, lds[3 * wave + 1] = s.S, lds[3 * wave + 2] = s.T;
+  __syncthreads();
+  float m = lds[0];
+  for (int w = 1; w < WAVES; ++w) m = fmaxf(m, lds[3 * w]);
   Sums r{m, 0.f, 0.f};
-  for (const Sums& x : {a, b}) {
-    if (x.m == -INFINITY) {
-      r.S += x.S;
-      continue;
-    }
-    const float d = x.m - m, f = __builtin_amdgcn_exp2f(d * LOG2E);
-    r.S += x.S * f;
-    r.T += (x.T + fmaxf(d, -200.f) * x.S) * f;
+  for (int w = 0; w < WAVES; ++w) {
+    const Sums x = moved({lds[3 * w], lds[3 * w + 1], lds[3 * w + 2]}, m);
+    r.S += x.S, r.T += x.T;
   }
   return r;
 }
-__device__ __forceinline__ Sums wave_join(Sums a) {
-  for (int o = 32; o > 0; o >>= 1) {
-    const Sums b{__shfl_xor(a.m, o), __shfl_xor(a.S, o), __shfl_xor(a.T, o)};
-    a = join(a, b);
+
+// The n best keys of a wavefront's stream; all lanes call together.
+struct Best {
+  u64* buf;  // LDS, CAND + STEP keys
+  int n, count;
+  u64 least;    // the n-th key: nothing below it matters (0: fewer than n so far)
+  float bound;  // logits below it cannot pass
+  __device__ __forceinline__ Best(u64* b, int n_) : buf(b), n(n_), count(0), least(0), bound(-INFINITY) {}
+  template <int SLOTS>
+  __device__ __forceinline__ void rank_and_place() {
+    const int lane = threadIdx.x & 63;
+    u64 k[SLOTS];
+    int rank[SLOTS];
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) {
+      k[i] = lane + 64 * i < count ? buf[lane + 64 * i] : 0;
+      rank[i] = 0;
+    }
+    if (lane < STEP) buf[count + lane] = 0;
+    wave_sync();
+    for (int j = 0; j < count; j += STEP) {
+      u64 o[STEP];
+#pragma unroll
+      for (int u = 0; u < STEP; ++u) o[u] = buf[j + u];
+#pragma unroll
+      for (int u = 0; u < STEP; ++u)
+#pragma unroll
+        for (int i = 0; i < SLOTS; ++i) rank[i] += o[u] > k[i];
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i)
+      if (lane + 64 * i < count && rank[i] < n) buf[rank[i]] = k[i];
+    wave_sync();
   }
-  return a;
+  __device__ __forceinline__ void cut() {
+    if (count <= 64) rank_and_place<1>();
+    else rank_and_place<CAND / 64>();
+    count = count < n ? count : n;
+    if (count == n) {
+      least = buf[n - 1];
+      bound = value_of(least);
+    }
+  }
+  // the keys of the lanes that have one (0: none)
+  __device__ __forceinline__ void add(u64 k) {
+    if (count > CAND - 64) cut();
+    const bool in = k > least;
+    const u64 mask = __ballot(in);
+    if (in) buf[count + __builtin_amdgcn_mbcnt_hi(mask >> 32, __builtin_amdgcn_mbcnt_lo(mask, 0))] = k;
+    count += __popcll(mask);
+  }
+  // LDS accesses of one wavefront run in order; this keeps the compiler to it
+  static __device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
+// the largest of the 16 lanes of a DPP row, in all of them
+__device__ __forceinline__ float row_max(float v) {
+  const auto with = [](float x, auto ctrl) {
+    return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(ctrl)::value, 0xf,
+                                                                0xf, true)));
+  };
+  v = with(v, std::integral_constant<int, 0x128>{});  // rotate by 8, 4, 2, 1
+  v = with(v, std::integral_constant<int, 0x124>{});
+  v = with(v, std::integral_constant<int, 0x122>{});
+  return with(v, std::integral_constant<int, 0x121>{});
 }
 
-// the row's results from its sums and its sorted top keys (thread 0 and the first n threads)
+// The n best of the wavefronts' lists, sorted, to top[0 .. n) (0: none left).
+__device__ __forceinline__ void block_top(Best& b, u64 (*bufs)[CAND + STEP], u64* top) {
+  b.cut();
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  if (lane >= b.count && lane < b.n + STEP) bufs[wave][lane] = 0;
+  if (t < 32) top[t] = 0;
+  __syncthreads();
+  for (int i = t; i < WAVES * b.n; i += THREADS) {
+    const u64 k = bufs[i / b.n][i % b.n];
+    int rank = 0;
+    for (int w = 0; w < WAVES; ++w)
+      for (int j = 0; j < b.n; j += STEP) {
+        u64 o[STEP];
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) o[u] = bufs[w][j + u];
+#pragma unroll
+        for (int u = 0; u < STEP; ++u) rank += o[u] > k;
+      }
+    if (k && rank < b.n) top[rank] = k;
+  }
+  __syncthreads();
+}
+
+// The n best of x[k] at index i0 + k step (-inf: none), over the wavefront, into b. `lanes`: groups
+// of lanes for the first call's bound.
+template <int K>
+__device__ __forceinline__ void consider(Best& b, const float (&x)[K], int i0, int step, bool first, int lanes) {
+  float hi = x[0];
+#pragma unroll
+  for (int k = 1; k < K; ++k) hi = fmaxf(hi, x[k]);
+  if (first) {
+    float g = hi;
+    for (int o = 32; o >= lanes; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
+    int higher = 0;
+    if (lanes == 64) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i)) > g;
+    } else {
+      for (int i = 0; i < lanes; ++i)
+        higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i)) > g;
+    }
+    b.bound = -wave_max(higher < b.n ? -g : -INFINITY);
+  }
+  if (!__any(hi >= b.bound && hi > -INFINITY)) return;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool in = x[k] >= b.bound && x[k] > -INFINITY;
+    if (__any(in)) b.add(in ? key_of(x[k], i0 + k * step) : 0);
+  }
+  if (first) b.cut();
+}
+
+// The row's results from its sums and its groups' maxima (LDS or workspace), by the whole workgroup.
 template <typename T>
-__device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, const u64* top) {
+__device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, const float* maxima, int lanes,
+                                       u64 (*bufs)[CAND + STEP], u64* top) {
+  constexpr int VE = 16 / sizeof(T), GT = GROUP * VE, PER = GT / 64;  // tokens of a group, of a lane
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.n_top;
+  const T* const x0 = (const T*)a.logits + row * a.ld;
   const bool bad = s.S != s.S, none = s.m == -INFINITY;
-  const float lnS = logf(s.S);
-  const int t = threadIdx.x;
+  const float l2 = log2f(s.S);
+  const auto logprob = [&](float x) {
+    return fabsf(x) < HUGE_X && fabsf(s.m) < HUGE_X ? (above(x, s.m) - l2) * LN2 : x - s.m - l2 * LN2;
+  };
   if (t == 0) {
-    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : lnS - s.T / s.S;
+    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : (l2 - s.T / s.S) * LN2;
     if (a.logprob) {
       const int tok = a.tokens[row];
       float r = 0.f;
       if (tok >= a.vocab || (tok >= 0 && bad))
         r = NAN;
       else if (tok >= 0)
-        r = none || tok == a.exclude ? -INFINITY : (float)((const T*)a.logits)[row * a.ld + tok] - s.m - lnS;
+        r = none || tok == a.exclude ? -INFINITY : logprob((float)x0[tok]);
       a.logprob[row] = r;
     }
   }
-  if (t < a.n_top) {
+  if (n == 0) return;
+  const int off = (int)(((uintptr_t)x0 / sizeof(T)) % VE);
+  const int groups = (off + a.vocab + GT - 1) / GT;
+  {
+    constexpr int K = 4;
+    Best b(bufs[wave], n);
+    for (int base = 0; base < groups; base += THREADS * K) {
+      float x[K];
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int i = base + k * THREADS + t;
+        x[k] = i < groups ? maxima[i] : -INFINITY;
+      }
+      consider(b, x, base + t, THREADS, base == 0, lanes);
+    }
+    block_top(b, bufs, top);
+  }
+  // the groups' logits: wavefront w has the groups w, w + 4, ...
+  constexpr int MINE = 32 / WAVES;
+  Best b(bufs[wave], n);
+  if (top[n - 1]) b.bound = value_of(top[n - 1]);
+  float y[MINE][PER];
+  int tok[MINE];
+#pragma unroll
+  for (int g = 0; g < MINE; ++g) {
+    const int at = wave + WAVES * g;
+    const u64 k = at < n ? top[at] : 0;
+    tok[g] = token_of(k) * GT + lane * PER - off;
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      y[g][e] = k && (unsigned)(tok[g] + e) < (unsigned)a.vocab && tok[g] + e != a.exclude ? (float)x0[tok[g] + e]
+                                                                                           : -INFINITY;
+  }
+  __syncthreads();  // the lists are read, their buffers are free
+#pragma unroll
+  for (int g = 0; g < MINE; ++g) consider(b, y[g], tok[g], 1, false, lanes);
+  block_top(b, bufs, top);
+  if (t < n) {
     const u64 k = top[t];
-    const int64_t at = (int64_t)row * a.n_top + t;
+    const int64_t at = (int64_t)row * n + t;
     a.top_ids[at] = bad || k == 0 ? -1 : token_of(k);
-    a.top_logprobs[at] = bad ? NAN : k == 0 ? -INFINITY : value_of(k) - s.m - lnS;
+    a.top_logprobs[at] = bad ? NAN : k == 0 ? -INFINITY : logprob(value_of(k));
   }
 }
 
-// Workspace: [rows][segs] Sums, then [rows][segs][n_top] keys.
+// Workspace: [rows][parts] Sums if parts > 1, then [rows][groups] maxima.
+__device__ __forceinline__ float* ws_maxima(const LogprobArgs& a, int parts, int row, int groups) {
+  return (float*)a.ws + (parts > 1 ? (int64_t)a.rows * parts * 3 : 0) + (int64_t)row * groups;
+}
+
 template <typename T, int NV>
-__global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobArgs a, int segs, int groups) {
+__global__ void __launch_bounds__(THREADS, 4)
+logprobs_kernel(LogprobArgs a, int segs, int parts, int groups, int lanes) {
   constexpr int VE = 16 / sizeof(T), EPT = NV * VE, SEG = THREADS * EPT;
   typedef T vec __attribute__((ext_vector_type(VE)));
-  __shared__ Sums part[WAVES];
-  __shared__ float bound[WAVES];
-  __shared__ u64 cand[CAND];
+  __shared__ float sums[3 * WAVES];
+  __shared__ u64 bufs[WAVES][CAND + STEP];
   __shared__ u64 top[32];
-  __shared__ int count;
-  const int row = blockIdx.x / segs, seg = blockIdx.x % segs, t = threadIdx.x;
+  extern __shared__ float lds_maxima[];
+  const int row = blockIdx.x / parts, part = blockIdx.x % parts, t = threadIdx.x;
+  const int seg0 = (int)((int64_t)segs * part / parts), seg1 = (int)((int64_t)segs * (part + 1) / parts);
   const T* const x0 = (const T*)a.logits + row * a.ld;
   // vectors are aligned in memory: the row starts `off` elements into its first one
   const int off = (int)(((uintptr_t)x0 / sizeof(T)) % VE);
-  const int first = seg * SEG + t * VE - off;  // token of this thread's first element
+  float* const maxima = parts == 1 && groups <= LDS_GROUPS ? lds_maxima : ws_maxima(a, parts, row, groups);
 
-  float x[EPT];
+  // Vectors outside the row are read as its last one and its edge vectors whole (16 aligned
+  // bytes that hold a logit of the row): no branch lies between the loads and their use a
+  // segment later. What is not the row's is set to -inf there.
+  const vec* const v0 = (const vec*)(x0 - off);
+  const int v_last = (off + a.vocab - 1) / VE;
+  vec next[NV];
+  const auto load = [&](int seg) {
+    const int v = seg * THREADS * NV + t;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int i = first + k * THREADS * VE;
-    if (i >= 0 && i + VE <= a.vocab) {
-      const vec v = *(const vec*)(x0 + i);
+    for (int k = 0; k < NV; ++k) next[k] = v0[v + k * THREADS < v_last ? v + k * THREADS : v_last];
+  };
+  Sums s{-INFINITY, 0.f, 0.f};
+  load(seg0);
+  for (int seg = seg0; seg < seg1; ++seg) {
+    const int first = seg * SEG + t * VE - off;  // token of this thread's first element
+    float x[EPT];
 #pragma unroll
-      for (int e = 0; e < VE; ++e) x[k * VE + e] = (float)v[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < VE; ++e)
-        x[k * VE + e] = i + e >= 0 && i + e < a.vocab ? (float)x0[i + e] : -INFINITY;
-    }
-  }
-  const int ex = a.exclude + off - seg * SEG;  // the excluded token's place in the segment
-  if (a.exclude >= 0 && ex >= 0 && ex < SEG) {
-#pragma unroll
-    for (int j = 0; j < EPT; ++j)
-      if (ex == (j / VE) * THREADS * VE + t * VE + j % VE) x[j] = -INFINITY;
-  }
-  float mine = -INFINITY;  // the largest of this thread
-#pragma unroll
-  for (int j = 0; j < EPT; ++j) mine = fmaxf(mine, x[j]);
-  Sums s{wave_max(mine), 0.f, 0.f};
-  {
-    const float m = s.m == -INFINITY ? 0.f : s.m;
-#pragma unroll
-    for (int j = 0; j < EPT; ++j) {
-      const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * LOG2E);
-      s.S += e;
-      s.T += fmaxf(d, -200.f) * e;  // -inf: no part (-200 x 0)
-    }
-    s.S = wave_sum(s.S), s.T = wave_sum(s.T);
-  }
-  const int lane = t & 63, wave = t >> 6;
-  if (a.n_top) {
-    // the n-th largest maximum of `groups` groups of lanes
-    float g = mine;
-    for (int o = 32; o >= groups; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
-    int above = 0;
-    for (int i = 0; i < groups; ++i)
-      above += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i)) > g;
-    float b = above < a.n_top ? g : INFINITY;
-    for (int o = 32; o > 0; o >>= 1) b = fminf(b, __shfl_xor(b, o));
-    if (lane == 0) bound[wave] = b;
-  }
-  if (lane == 0) part[wave] = s;
-  if (t == 0) count = 0;
-  if (t < 32) top[t] = 0;
-  __syncthreads();
-  s = part[0];
-  for (int w = 1; w < WAVES; ++w) s = join(s, part[w]);
-  if (a.n_top) {
-    float b = bound[0];
-    for (int w = 1; w < WAVES; ++w) b = fmaxf(b, bound[w]);
-    if (mine >= b && mine > -INFINITY) {
+    for (int j = 0; j < EPT; ++j) x[j] = (float)next[j / VE][j % VE];
+    if (seg + 1 < seg1) load(seg + 1);
+    if (seg * SEG < off || (seg + 1) * SEG > off + a.vocab) {
 #pragma unroll
       for (int j = 0; j < EPT; ++j)
-        if (x[j] >= b && x[j] > -INFINITY) {
-          const int at = atomicAdd(&count, 1);
-          if (at < CAND) cand[at] = key_of(x[j], first + (j / VE) * THREADS * VE + j % VE);
-        }
+        if ((unsigned)(first + (j / VE) * THREADS * VE + j % VE) >= (unsigned)a.vocab) x[j] = -INFINITY;
     }
-    __syncthreads();
-    const int n = count;
-    if (n <= CAND) {
-      for (int i = t; i < n; i += THREADS) {
-        const u64 k = cand[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += cand[j] > k;
-        if (rank < a.n_top) top[rank] = k;
-      }
-    } else {
-      u64 last = ~0ull;
-      for (int r = 0; r < a.n_top && last; ++r) {
-        u64 best = 0;
+    const int ex = a.exclude + off - seg * SEG;  // the excluded token's place in the segment
+    if (a.exclude >= 0 && ex >= 0 && ex < SEG) {
+#pragma unroll
+      for (int j = 0; j < EPT; ++j)
+        if (ex == (j / VE) * THREADS * VE + t * VE + j % VE) x[j] = -INFINITY;
+    }
+    float vhi[NV], hi = -INFINITY, lo = INFINITY;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      vhi[k] = x[k * VE];
+#pragma unroll
+      for (int e = 1; e < VE; ++e) vhi[k] = fmaxf(vhi[k], x[k * VE + e]);
+      hi = fmaxf(hi, vhi[k]);
+    }
+#pragma unroll
+    for (int j = 0; j < EPT; ++j) lo = fminf(lo, x[j]);
+    if (hi > s.m) s = moved(s, hi);
+    {
+      const float m = s.m == -INFINITY ? 0.f : s.m;
+      float S = 0.f, M = 0.f;  // of the segment: short sums
+      if (!__any(lo < -HUGE_X || fabsf(m) >= HUGE_X)) {
+        const float r = m * LOG2E;
 #pragma unroll
         for (int j = 0; j < EPT; ++j) {
-          const u64 k = x[j] > -INFINITY ? key_of(x[j], first + (j / VE) * THREADS * VE + j % VE) : 0;
-          if (k < last && k > best) best = k;
+          const float d = fmaf(x[j], LOG2E, -r), e = __builtin_amdgcn_exp2f(d);
+          S += e;
+          M = fmaf(d, e, M);
         }
-        for (int o = 32; o > 0; o >>= 1) {
-          const u64 k = __shfl_xor(best, o);
-          best = k > best ? k : best;
+      } else {
+#pragma unroll
+        for (int j = 0; j < EPT; ++j) {
+          const float d = above(x[j], m), e = __builtin_amdgcn_exp2f(d);
+          S += e;
+          M = fmaf(fmaxf(d, -300.f), e, M);  // -inf: no part (-300 x 0)
         }
-        __syncthreads();
-        if (lane == 0) cand[wave] = best;
-        __syncthreads();
-        last = cand[0];
-        for (int w = 1; w < WAVES; ++w) last = cand[w] > last ? cand[w] : last;
-        if (t == 0) top[r] = last;
+      }
+      s.S += S, s.T += M;
+    }
+    if (a.n_top) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const float g = row_max(vhi[k]);
+        const int i = (seg * NV + k) * (THREADS / GROUP) + t / GROUP;
+        if (t % GROUP == 0 && i < groups) maxima[i] = g;
       }
     }
-    __syncthreads();
   }
-  if (segs == 1) {
-    finish<T>(a, row, s, top);
+  s = block_sums(s, sums);
+  if (parts == 1) {
+    finish<T>(a, row, s, maxima, lanes, bufs, top);
     return;
   }
-  const int64_t at = (int64_t)row * segs + seg;
-  if (t == 0) ((Sums*)a.ws)[at] = s;
-  u64* keys = (u64*)((char*)a.ws + (((int64_t)a.rows * segs * sizeof(Sums) + 15) & ~(int64_t)15));
-  if (t < a.n_top) keys[at * a.n_top + t] = top[t];
+  if (t == 0) ((Sums*)a.ws)[(int64_t)row * parts + part] = s;
 }
 
-// Joins a row's segments: one workgroup per row.
+// Joins a row's parts: one workgroup per row.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) logprobs_join_kernel(LogprobArgs a, int segs) {
-  __shared__ Sums part[WAVES];
-  __shared__ u64 list[LISTS * 32];
+__global__ void __launch_bounds__(THREADS) logprobs_join_kernel(LogprobArgs a, int parts, int groups, int lanes) {
+  __shared__ float sums[3 * WAVES];
+  __shared__ u64 bufs[WAVES][CAND + STEP];
   __shared__ u64 top[32];
-  const int row = blockIdx.x, t = threadIdx.x, n = a.n_top;
-  const Sums* const sums = (const Sums*)a.ws + (int64_t)row * segs;
-  const u64* const keys = (const u64*)((const char*)a.ws +
-                                       (((int64_t)a.rows * segs * sizeof(Sums) + 15) & ~(int64_t)15)) +
-                          (int64_t)row * segs * n;
+  const int row = blockIdx.x, t = threadIdx.x;
   Sums s{-INFINITY, 0.f, 0.f};
-  for (int i = t; i < segs; i += THREADS) s = join(s, sums[i]);
-  s = wave_join(s);
-  if ((t & 63) == 0) part[t >> 6] = s;
-  if (t < 32) top[t] = 0;
-  __syncthreads();
-  s = part[0];
-  for (int w = 1; w < WAVES; ++w) s = join(s, part[w]);
-  // sorted lists of n keys, the result so far as list 0: a key's rank is the number of
-  // larger ones, by bisection in every list
-  for (int base = 0; n && base < segs; base += LISTS - 1) {
-    const int lists = 1 + (segs - base < LISTS - 1 ? segs - base : LISTS - 1);
-    for (int i = t; i < lists * n; i += THREADS) list[i] = i < n ? top[i] : keys[(int64_t)base * n + i - n];
-    __syncthreads();
-    if (t < 32) top[t] = 0;
-    __syncthreads();
-    for (int i = t; i < lists * n; i += THREADS) {
-      const u64 k = list[i];
-      if (k == 0) continue;
-      int rank = 0;
-      for (int j = 0; j < lists && rank < n; ++j) {
-        int lo = 0, hi = n;  // keys of list j above k
-        while (lo < hi) {
-          const int mid = (lo + hi) >> 1;
-          if (list[j * n + mid] > k) lo = mid + 1;
-          else hi = mid;
-        }
-        rank += lo;
-      }
-      if (rank < n) top[rank] = k;
-    }
-    __syncthreads();
-  }
-  finish<T>(a, row, s, top);
+  if (t < parts) s = ((const Sums*)a.ws)[(int64_t)row * parts + t];
+  s = block_sums(s, sums);
+  finish<T>(a, row, s, ws_maxima(a, parts, row, groups), lanes, bufs, top);
+}
+
+int64_t groups_of(int64_t vocab, int elem) {
+  const int64_t ve = 16 / elem;
+  return (vocab + ve - 1 + GROUP * ve - 1) / (GROUP * ve);
 }
 
 int64_t segments(int64_t vocab, int nv, int elem) {
@@ -264,45 +406,60 @@ int64_t segments(int64_t vocab, int nv, int elem) {
   return (vocab + ve - 1 + seg - 1) / seg;
 }
 
-// Few segments in all: short ones (2 vectors a thread), so that more compute units share
-// the rows.
-int vectors(int64_t rows, int64_t vocab, int elem) { return rows * segments(vocab, 8, elem) >= 512 ? 8 : 2; }
+struct Cut {
+  int nv, segs, parts;
+};
+// How rows are cut: long segments (4 vectors a thread) unless those leave compute units
+// without one, and the parts that end soonest with WGS workgroups at a time (a row's
+// joining counts as one segment).
+Cut cut_rows(int64_t rows, int64_t vocab, int elem) {
+  constexpr int64_t WGS = 256 * 4;
+  Cut c{};
+  c.nv = rows * segments(vocab, 4, elem) >= 256 ? 4 : 1;
+  c.segs = (int)segments(vocab, c.nv, elem);
+  int64_t least = INT64_MAX;
+  for (int p = 1; p <= c.segs && p <= PARTS; ++p) {
+    const int64_t rounds = (rows * p + WGS - 1) / WGS, cost = rounds * ((c.segs + p - 1) / p) + (p > 1);
+    if (cost < least) least = cost, c.parts = p;
+    if (rounds > 1 && p >= 8) break;
+  }
+  return c;
+}
 
 template <typename T, int NV>
-hipError_t launch(const LogprobArgs& a, int segs, hipStream_t s) {
-  const int64_t n = (int64_t)a.rows * segs;
-  int groups = 1;  // at least twice n where the lanes allow it
-  while (groups < 64 && groups < 2 * a.n_top) groups *= 2;
-  logprobs_kernel<T, NV><<<dim3((unsigned)n), dim3(THREADS), 0, s>>>(a, segs, groups);
+hipError_t launch(const LogprobArgs& a, const Cut& c, hipStream_t s) {
+  int lanes = 1;  // at least twice n where there are as many
+  while (lanes < 64 && lanes < 2 * a.n_top) lanes *= 2;
+  const int groups = (int)groups_of(a.vocab, sizeof(T));
+  const int lds = a.n_top && c.parts == 1 && groups <= LDS_GROUPS ? groups * 4 : 0;
+  logprobs_kernel<T, NV><<<dim3((unsigned)a.rows * c.parts), dim3(THREADS), lds, s>>>(a, c.segs, c.parts, groups, lanes);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || segs == 1) return e;
-  logprobs_join_kernel<T><<<dim3(a.rows), dim3(THREADS), 0, s>>>(a, segs);
+  if (e != hipSuccess || c.parts == 1) return e;
+  logprobs_join_kernel<T><<<dim3(a.rows), dim3(THREADS), 0, s>>>(a, c.parts, groups, lanes);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_type(const LogprobArgs& a, hipStream_t s) {
-  const int nv = vectors(a.rows, a.vocab, sizeof(T));
-  const int segs = (int)segments(a.vocab, nv, sizeof(T));
-  return nv == 8 ? launch<T, 8>(a, segs, s) : launch<T, 2>(a, segs, s);
+  const Cut c = cut_rows(a.rows, a.vocab, sizeof(T));
+  return c.nv == 4 ? launch<T, 4>(a, c, s) : launch<T, 1>(a, c, s);
 }
 
 }  // namespace
 
 // The type is not among the sizes: the larger of the two.
-LogprobPlan logprobs_plan(int rows, int vocab, int n_top) {
-  LogprobPlan p{};
+int64_t logprobs_workspace(int rows, int vocab, int n_top) {
+  int64_t most = 0;
   for (int elem : {2, 4}) {
-    const int64_t segs = segments(vocab, vectors(rows, vocab, elem), elem);
-    const int64_t bytes =
-        segs == 1 ? 0 : ((rows * segs * (int64_t)sizeof(Sums) + 15) & ~(int64_t)15) + rows * segs * n_top * 8;
-    p.bytes = bytes > p.bytes ? bytes : p.bytes;
-    p.workgroups = rows * segs > p.workgroups ? rows * segs : p.workgroups;
+    const int64_t parts = rows ? cut_rows(rows, vocab, elem).parts : 1, groups = groups_of(vocab, elem);
+    const bool maxima = n_top && (parts > 1 || groups > LDS_GROUPS);
+    const int64_t bytes = 4 * rows * ((parts > 1 ? 3 * parts : 0) + (maxima ? groups : 0));
+    most = bytes > most ? bytes : most;
   }
-  return p;
+  return most;
 }
 
-hipError_t launch_token_logprobs(const LogprobArgs& a, const LogprobPlan&, hipStream_t s) {
+hipError_t launch_token_logprobs(const LogprobArgs& a, hipStream_t s) {
   if (a.dtype == LOPA_BF16) return launch_type<__bf16>(a, s);
   if (a.dtype == LOPA_F16) return launch_type<_Float16>(a, s);
   return launch_type<float>(a, s);

@@ -169,10 +169,7 @@ int64_t lopa_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top
       n_top > LOPA_MAX_TOP)
     return lopa_fail(LOPA_ESHAPE, "rows %d, vocab %d or n_top %d outside [0, 2^24], [1, 2^24], [0, %d]",
                      rows, vocab, n_top, LOPA_MAX_TOP);
-  const LogprobPlan p = logprobs_plan(rows, vocab, n_top);
-  if (p.workgroups >= ((int64_t)1 << 31))
-    return lopa_fail(LOPA_ESHAPE, "%d rows of %d logits are too many for one call", rows, vocab);
-  return p.bytes;
+  return logprobs_workspace(rows, vocab, n_top);
 }
 
 int lopa_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int32_t rows,
@@ -208,8 +205,7 @@ int lopa_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int32_t r
   a.exclude = exclude, a.tokens = tokens, a.n_top = n_top;
   a.logprob = logprob, a.entropy = entropy, a.top_ids = top_ids, a.top_logprobs = top_logprobs;
   a.ws = workspace;
-  return launched(launch_token_logprobs(a, logprobs_plan(rows, vocab, n_top), (hipStream_t)stream),
-                  "token logprobs");
+  return launched(launch_token_logprobs(a, (hipStream_t)stream), "token logprobs");
 }
 
 }  // extern "C"

@@ -371,6 +371,23 @@ def test_logprobs_masked_rows(lp, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF, F32])
+def test_logprobs_late_extremes(lp, dtype):
+    """The largest logits, the type's largest, NaN runs and -inf runs late in a long row, after
+    thousands of ordinary ones; one row of NaN only."""
+    V = 70000
+    x = randn(3, (6, V), dtype, 2.0)
+    x[0, 69990:] = torch.arange(10, device="cuda").to(dtype) * 3 + 20
+    x[1, 50000] = torch.finfo(dtype).max
+    x[2, 40000:60000] = math.nan
+    x[3, 20000:] = -math.inf
+    x[4] = math.nan
+    x[5, :69000] = -math.inf
+    tokens = torch.tensor([69999, 50000, 1, 30000, 3, 69999], dtype=I32, device="cuda")
+    check_score(lp, x, tokens, -1, 20)
+    check_score(lp, x[:, 1:], tokens - 1, 69998, 3)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, F32])
 @pytest.mark.parametrize("offset,pad", [(0, 0), (1, 0), (3, 5), (7, 1)])
 def test_logprobs_strides(lp, dtype, offset, pad):
     """Rows that start at any element (odd vocabularies, views), and rows far apart."""
