@@ -18,7 +18,8 @@ SOURCES = ["api.cpp", "step_kernels.hip", "row_kernels.hip", "gemm.hip", "attent
            "noalloc.hip", "serving_api.cpp", "paged_append.hip", "paged_attention.hip", "logprobs.hip"]
 # attention: scores are never NaN, and without NaN semantics the maximum of
 # scores needs no quieting of its operands
-EXTRA_FLAGS = {"attention.hip": ["-fno-honor-nans"]}
+# (paged: a NaN only passes through products, sums and exponentials there)
+EXTRA_FLAGS = {"attention.hip": ["-fno-honor-nans"], "paged_attention.hip": ["-fno-honor-nans"]}
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          # no packed-fp32 instructions in device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -227,6 +227,7 @@ struct PagedAttnArgs {
   lopa_pages pages;
   lopa_paged_batch batch;
   int heads, max_rows, max_len;
+  int page_shift;  // page_size = 1 << page_shift
   const void* q;
   void* out;
   int64_t ld_q, ld_out;

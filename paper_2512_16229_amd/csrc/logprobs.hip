@@ -26,8 +26,6 @@
 #include "common.h"
 #include "kernels.h"
 
-#include <type_traits>
-
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
@@ -149,16 +147,19 @@ struct Best {
   }
 };
 
-// the largest of the 16 lanes of a DPP row, in all of them
-__device__ __forceinline__ float row_max(float v) {
-  const auto with = [](float x, auto ctrl) {
-    return fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(ctrl)::value, 0xf,
-                                                                0xf, true)));
-  };
-  v = with(v, std::integral_constant<int, 0x128>{});  // rotate by 8, 4, 2, 1
-  v = with(v, std::integral_constant<int, 0x124>{});
-  v = with(v, std::integral_constant<int, 0x122>{});
-  return with(v, std::integral_constant<int, 0x121>{});
+// v[k] becomes the largest of its 16 lanes of a DPP row, in all of them
+template <int CTRL, int K>
+__device__ __forceinline__ void row_max_step(float (&v)[K]) {
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+    v[k] = fmaxf(v[k], __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v[k]), CTRL, 0xf, 0xf, true)));
+}
+template <int K>
+__device__ __forceinline__ void row_max(float (&v)[K]) {
+  row_max_step<0x128>(v);  // rotations by 8, 4, 2, 1
+  row_max_step<0x124>(v);
+  row_max_step<0x122>(v);
+  row_max_step<0x121>(v);
 }
 
 // The n best of the wavefronts' lists, sorted, to top[0 .. n) (0: none left).
@@ -366,11 +367,11 @@ logprobs_kernel(LogprobArgs a, int segs, int parts, int groups, int lanes) {
       s.S += S, s.T += M;
     }
     if (a.n_top) {
+      row_max(vhi);
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
-        const float g = row_max(vhi[k]);
         const int i = (seg * NV + k) * (THREADS / GROUP) + t / GROUP;
-        if (t % GROUP == 0 && i < groups) maxima[i] = g;
+        if (t % GROUP == 0 && i < groups) maxima[i] = vhi[k];
       }
     }
   }

@@ -15,8 +15,7 @@
 // keys may be taken in any order, so the keys of a step are those a lane has). V^T's
 // operand comes from the row-major V by the transposing LDS read.
 //
-// K / V tiles go global -> LDS without registers, double-buffered: the copies of tile
-// i + 1 are in flight while tile i is computed. 16-byte chunks of a row are stored
+// K / V tiles go global -> LDS without registers, double-buffered. 16-byte chunks of a row are stored
 // permuted by the row (`swz`), so that the reads of 32 rows and the transposing reads
 // of 4 rows touch different banks; the permutation is in the copy's global address.
 //
@@ -29,6 +28,7 @@
 
 namespace {
 
+constexpr float LOG2E = 1.44269504f;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
@@ -125,8 +125,10 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   constexpr int WK = Shape<WM>::WK, BM = Shape<WM>::BM, KT = Shape<WM>::KT, NB = KT / 32;
   constexpr int TILE = KT * D * 2, STAGE = 2 * TILE;     // bytes of K or V, of both
   constexpr int GROUPS = KT / 16, MYG = WM == 4 ? 1 : 2; // 16-row groups of a tile, a wavefront's
+  constexpr uint32_t ALL = (1u << GROUPS) - 1;
   constexpr int RPI = 512 / D, IPG = 16 / RPI;           // rows of a copy, copies of a group
   extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ int put_back[1];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -170,16 +172,17 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   const int lim_min = idle ? 0 : key_limit(pos0 + w0 / G, a.block, q.len);
   const int lim_max = idle ? 0 : key_limit(pos0 + ((w0 + 31 < m1 ? w0 + 31 : m1 - 1)) / G, a.block, q.len);
 
+  // scores in units of log2: x = sc (q . K), the sign of the scale in q; a scale of 0 is q = 0
+  const float sc = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
   vec8 qf[D / 16];
   {
     const T* qp = (const T*)a.q + row * a.ld_q + head * D + 8 * h;
 #pragma unroll
-    for (int st = 0; st < D / 16; ++st) qf[st] = *(const vec8*)(qp + 16 * st);
-    if (a.scale < 0.f)
-#pragma unroll
-      for (int st = 0; st < D / 16; ++st) qf[st] = -qf[st];
+    for (int st = 0; st < D / 16; ++st) {
+      qf[st] = *(const vec8*)(qp + 16 * st);
+      if (a.scale <= 0.f) qf[st] = a.scale == 0.f ? vec8{} : -qf[st];
+    }
   }
-  const float sc = fabsf(a.scale) * 1.44269504f;
 
   // copies: this lane's offset inside a 16-row group
   uint32_t voff[IPG];
@@ -188,7 +191,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     const int r = RPI * i + lane / (D / 8);
     voff[i] = r * D * 2 + (((lane % (D / 8)) ^ swz<D>(r)) << 4);
   }
-  const uint32_t ring = lds0 + wk * 2 * STAGE;
+  const uint32_t k_ring = lds0 + wk * 2 * STAGE, v_ring = k_ring + 2 * TILE;
   const int64_t page_elems = (int64_t)Hkv * ps * D;
   const T* const kbase = (const T*)a.pages.k + (int64_t)kvh * ps * D;
   const T* const vbase = (const T*)a.pages.v + (int64_t)kvh * ps * D;
@@ -197,26 +200,56 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   // the pages of a tile: lane j < GROUPS reads that of 16-key group j (-1: none there)
   const int first = k0 / KT + wk, last = (k1 + KT - 1) / KT;  // key tiles first, first + WK, ... < last
   const int iters = (last - k0 / KT + WK - 1) / WK;
-  auto page_of = [&](int t) {
-    const int p = t * KT + 16 * (lane % GROUPS);
-    return p < k1 ? table[p / ps] : -1;
+  const auto page_of = [&](int it) {
+    const int p = (first + it * WK) * KT + 16 * (lane % GROUPS);
+    return it < iters && p < k1 ? table[p >> a.page_shift] : -1;
   };
-  auto issue = [&](int t, int ids, int buf) {
+  const auto there = [&](int ids) {  // bit j: group j has a page
+    return (uint32_t)(__ballot(ids >= 0 && ids < a.pages.n_pages) & ALL);
+  };
+  const auto copy = [&](const T* from, uint32_t ring, int it, int ids) {
 #pragma unroll
     for (int g = 0; g < MYG; ++g) {
       const int j = WM == 1 ? g : WM == 2 ? 2 * wm + g : wm;
       const int id = __builtin_amdgcn_readlane(ids, j);
       const bool ok = id >= 0 && id < a.pages.n_pages;
-      const int64_t off = ok ? id * page_elems + (int64_t)((t * KT + 16 * j) % ps) * D : 0;
-      const uint32_t to = ring + buf * STAGE + j * 16 * D * 2;
+      const int64_t off = ok ? id * page_elems + (int64_t)(((first + it * WK) * KT + 16 * j) & (ps - 1)) * D : 0;
+      const uint32_t to = ring + (it & 1) * TILE + j * 16 * D * 2;
 #pragma unroll
-      for (int i = 0; i < IPG; ++i) copy_to_lds(kbase + off, voff[i], to + i * 1024);
-#pragma unroll
-      for (int i = 0; i < IPG; ++i) copy_to_lds(vbase + off, voff[i], to + TILE + i * 1024);
+      for (int i = 0; i < IPG; ++i) copy_to_lds(from + off, voff[i], to + i * 1024);
     }
   };
-  auto there = [&](int ids) {  // bit j: group j has a page
-    return (uint32_t)(__ballot(ids >= 0 && ids < a.pages.n_pages) & ((1u << GROUPS) - 1));
+  // A value of V that is not finite would reach rows that do not see its key as 0 x infinity.
+  // Where a tile hides keys from some row of the workgroup such values are taken as zeros, by
+  // the wavefront that copied them, and put back after the loop for the rows that see them.
+  const int lim_first = key_limit(pos0 + m0 / G, a.block, q.len);  // of the tile's first row
+  const auto hides = [&](int it, uint32_t have) {
+    return have != ALL || (first + it * WK + 1) * KT > lim_first;
+  };
+  if (threadIdx.x == 0) *put_back = 0;
+  __syncthreads();
+  const auto make_finite = [&](int it) {
+    for (int g = 0; g < MYG; ++g) {
+      const int j = WM == 1 ? g : WM == 2 ? 2 * wm + g : wm;
+      const uint32_t at = v_ring + (it & 1) * TILE + j * 16 * D * 2 + lane * 16;
+#pragma unroll
+      for (int i = 0; i < IPG; ++i) {
+        u32x4 v = *LDS_PTR(u32x4, at + i * 1024);
+        u16x2 any = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) any |= over_finite<T>(v[k]);
+        if (__builtin_bit_cast(uint32_t, any) != 0) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const u16x2 d = over_finite<T>(v[k]);
+            if (d[0]) v[k] &= 0xffff0000u;
+            if (d[1]) v[k] &= 0xffffu;
+          }
+          *LDS_PTR(u32x4, at + i * 1024) = v;
+          *put_back = 1;
+        }
+      }
+    }
   };
 
   f32x16 o[D / 32];
@@ -225,14 +258,13 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float ref = -INFINITY, l = 0.f;
-  bool put_back = false;
 
-  // LDS addresses inside a stage: K rows by chunk step, V by (dimension block, key half)
+  // LDS addresses inside a tile: K rows by chunk step, V by (dimension block, key half)
   const uint32_t k_row = c * D * 2, k_swz = (h ^ swz<D>(c)) << 4;
   const int v_r = 4 * h + ((lane & 15) >> 2);
-  const uint32_t v_row = TILE + v_r * D * 2 + 8 * (lane & 1);
+  const uint32_t v_row = v_r * D * 2 + 8 * (lane & 1);
   const uint32_t v_swz = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz<D>(v_r)) << 4;
-  auto read_v = [&](uint32_t base, int t, int db) {
+  const auto read_v = [&](uint32_t base, int t, int db) {
     const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
         LDS_PTR(s16x4, base + v_row + (v_swz ^ (db << 6)) + t * 16 * D * 2));
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -240,153 +272,125 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(vec8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
+  const auto scores = [&](int it, f32x16 (&x)[NB]) {
+    const uint32_t base = k_ring + (it & 1) * TILE + k_row;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[nb][i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const u32x4 kf = *LDS_PTR(u32x4, base + (k_swz ^ (st << 5)) + nb * 32 * D * 2);
+        x[nb] = N::mfma(__builtin_bit_cast(vec8, kf), qf[st], x[nb]);
+      }
+  };
 
-  int ids = iters > 0 ? page_of(first) : -1;
-  uint32_t have = there(ids);
-  if (iters > 0) issue(first, ids, 0);
-  ids = iters > 1 ? page_of(first + WK) : -1;
-  for (int it = 0; it < iters; ++it) {
-    const int t = first + it * WK;
+  // Pipeline: iteration i multiplies K of tile i + 1 while it takes the exponentials of tile i,
+  // then V of tile i; the copies of K of tile i + 2 and V of tile i + 1 are in flight meanwhile.
+  f32x16 x[NB];
+  uint32_t have = 0;
+  int ids1 = -1, ids2 = -1;  // pages of tiles it + 1 and it + 2
+  if (iters > 0) {
+    const int ids0 = page_of(0);
+    ids1 = page_of(1);
+    have = there(ids0);
+    copy(kbase, k_ring, 0, ids0);
+    copy(vbase, v_ring, 0, ids0);
+    if (iters > 1) copy(kbase, k_ring, 1, ids1);
+    ids2 = page_of(2);
     wait_loads();
+    if constexpr (WM > 1) lds_barrier();
+    scores(0, x);
+  }
+  for (int it = 0; it < iters; ++it) {
+    wait_loads();
+    if (hides(it, have)) make_finite(it);
     if constexpr (WM > 1)
-      lds_barrier();  // every wavefront's copies of tile it have landed, tile it - 1 is done with
+      lds_barrier();  // every wavefront's copies have landed, and it is done with the tiles before
     else
       wait_lds();
-    uint32_t have_next = 0;
-    if (it + 1 < iters) {
-      have_next = there(ids);
-      issue(t + WK, ids, (it + 1) & 1);
-      ids = it + 2 < iters ? page_of(t + 2 * WK) : -1;
+    const uint32_t have_next = there(ids1);
+    if (it + 2 < iters) copy(kbase, k_ring, it + 2, ids2);
+    if (it + 1 < iters) copy(vbase, v_ring, it + 1, ids1);
+    ids1 = ids2;
+    ids2 = page_of(it + 3);
+    const int kt = (first + it * WK) * KT;
+    if constexpr (CAP) {
+      // log2(e) cap tanh(s / cap), tanh(y) = 1 - 2 / (e^(2y) + 1)
+      const float in = 2.f * sc / a.softcap, out = LOG2E * a.softcap;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          x[nb][i] = out - 2.f * out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[nb][i] * in) + 1.f);
     }
-    const int kt = t * KT;
-    if (kt < lim_max) {
-      const uint32_t base = ring + (it & 1) * STAGE;
-      f32x16 x[NB];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[nb][i] = 0.f;
-#pragma unroll
-      for (int st = 0; st < D / 16; ++st)
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const u32x4 kf = *LDS_PTR(u32x4, base + k_row + (k_swz ^ (st << 5)) + nb * 32 * D * 2);
-          x[nb] = N::mfma(__builtin_bit_cast(vec8, kf), qf[st], x[nb]);
-        }
-      if constexpr (CAP) {
-        // log2(e) cap tanh(s / cap), tanh(y) = 1 - 2 / (e^(2y) + 1); a NaN stays one
-        const float in = 2.f * sc / a.softcap, out = 1.44269504f * a.softcap;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            x[nb][i] = out - 2.f * out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[nb][i] * in) + 1.f);
-      } else {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x[nb][i] *= sc;
-      }
-      const bool clean = have == (1u << GROUPS) - 1 && kt + KT <= lim_min;
-      if (!clean) {
-        // hidden keys: those at or past the row's limit and those of missing pages
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int grp = nb * 2 + i / 8;
-            const int end = (have >> grp) & 1 ? lim - kt - 4 * h : INT32_MIN;
-            if (nb * 32 + 8 * (i / 4) + i % 4 >= end) x[nb][i] = -INFINITY;
-          }
-      }
-      float mt = x[0][0];
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, x[nb][i]);
-      mt = max_halves(mt);
-      if (__any(mt > ref + N::LIM)) {
-        const float next = mt > ref + N::LIM ? mt - N::SHIFT : ref;
-        const float f = ref == next ? 1.f : __builtin_amdgcn_exp2f(ref - next);
-        l *= f;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] *= f;
-        ref = next;
-      }
-      const float r = ref == -INFINITY ? 0.f : ref;  // no key seen so far
-      vec8 pf[2 * NB];
+    const float mul = CAP ? 1.f : sc;
+    if (have != ALL || kt + KT > lim_min) {
+      // hidden keys: those at or past the row's limit and those of missing pages
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float p = __builtin_amdgcn_exp2f(x[nb][i] - r);
-          l += p;
-          pf[2 * nb + i / 8][i % 8] = (T)p;
+          const int grp = nb * 2 + i / 8;
+          const int end = (have >> grp) & 1 ? lim - kt - 4 * h : INT32_MIN;
+          if (nb * 32 + 8 * (i / 4) + i % 4 >= end) x[nb][i] = -INFINITY;
         }
-      // A value of V that is not finite would reach the rows that do not see its key as
-      // 0 x infinity. Where a tile hides keys from some row such values are taken as zeros
-      // here and put back after the loop for the rows that see them.
-      bool odd = false;
-      if (!clean) {
-        u16x2 any = {};
-#pragma nounroll
-        for (int tt = 0; tt < 2 * NB; ++tt)
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) {
-            const u32x4 v = __builtin_bit_cast(u32x4, read_v(base, tt, db));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) any |= over_finite<T>(v[j]);
-          }
-        odd = __any(__builtin_bit_cast(uint32_t, any) != 0);
-      }
-      if (!odd) {
-#pragma unroll
-        for (int tt = 0; tt < 2 * NB; ++tt)
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) o[db] = N::mfma(read_v(base, tt, db), pf[tt], o[db]);
-      } else {
-        put_back = true;
-#pragma nounroll
-        for (int tt = 0; tt < 2 * NB; ++tt) {
-          vec8 p = pf[0];
-#pragma unroll
-          for (int k = 1; k < 2 * NB; ++k)
-            if (k == tt) p = pf[k];
-#pragma unroll
-          for (int db = 0; db < D / 32; ++db) {
-            u32x4 v = __builtin_bit_cast(u32x4, read_v(base, tt, db));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const u16x2 d = over_finite<T>(v[j]);
-              if (d[0]) v[j] &= 0xffff0000u;
-              if (d[1]) v[j] &= 0xffffu;
-            }
-            o[db] = N::mfma(__builtin_bit_cast(vec8, v), p, o[db]);
-          }
-        }
-      }
     }
+    float mt = x[0][0];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mt = fmaxf(mt, x[nb][i]);
+    mt = max_halves(mt) * mul;
+    if (__any(mt > ref + N::LIM)) {
+      const float next = mt > ref + N::LIM ? mt - N::SHIFT : ref;
+      const float f = ref == next ? 1.f : __builtin_amdgcn_exp2f(ref - next);
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= f;
+      ref = next;
+    }
+    const float r = ref == -INFINITY ? 0.f : ref;  // no key seen so far
+    f32x16 xn[NB];
+    scores(it + 1, xn);  // past the last tile: of what the buffer holds, not used
+    vec8 pf[2 * NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(x[nb][i], mul, -r));
+        l += p;
+        pf[2 * nb + i / 8][i % 8] = (T)p;
+      }
+    const uint32_t vb = v_ring + (it & 1) * TILE;
+#pragma unroll
+    for (int tt = 0; tt < 2 * NB; ++tt)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) o[db] = N::mfma(read_v(vb, tt, db), pf[tt], o[db]);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) x[nb] = xn[nb];
     have = have_next;
   }
   l = sum_halves(l);
-  if (put_back) {
-    // the wavefront's tiles in which some row has hidden keys: infinities and NaN of V, to
-    // the rows that see them
+  __syncthreads();  // put_back is known
+  if (*put_back) {
     for (int it = 0; it < iters; ++it) {
+      if (!hides(it, there(page_of(it)))) continue;
       const int kt = (first + it * WK) * KT;
       for (int p = kt; p < kt + KT && p < lim_max && p < k1; ++p) {
-        const int id = table[p / ps];
+        const int id = table[p >> a.page_shift];
         if (id < 0 || id >= a.pages.n_pages) continue;
-        if (kt + KT <= lim_min && there(page_of(first + it * WK)) == (1u << GROUPS) - 1) break;
-        const T* v = vbase + id * page_elems + (int64_t)(p % ps) * D + 4 * h;
+        const uint16_t* v = (const uint16_t*)vbase + id * page_elems + (int64_t)(p & (ps - 1)) * D + 4 * h;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float y = (float)v[32 * db + 8 * (i / 4) + i % 4];
-            if (p < lim && !(fabsf(y) < INFINITY)) o[db][i] += y;
+            const uint16_t y = v[32 * db + 8 * (i / 4) + i % 4];
+            if (p < lim && (y & 0x7fff) > N::MAX) o[db][i] += (float)__builtin_bit_cast(T, y);
           }
       }
     }
@@ -436,7 +440,6 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     constexpr int LD = D + 4;
     float* const so = (float*)smem;          // [WK][BM][LD]
     float* const sr = so + WK * BM * LD;     // [WK][BM][2]
-    wait_loads();
     __syncthreads();
     {
       float* p = so + (wk * BM + 32 * wm + c) * LD + 4 * h;

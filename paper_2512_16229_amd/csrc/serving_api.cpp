@@ -156,6 +156,7 @@ int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch,
   a.batch = *batch;
   a.heads = heads;
   a.max_rows = max_rows, a.max_len = max_len;
+  a.page_shift = __builtin_ctz(pages->page_size);
   a.q = q, a.out = out, a.ld_q = ld_q, a.ld_out = ld_out;
   a.block = block;
   a.scale = scale, a.softcap = softcap;
