@@ -26,6 +26,9 @@
 // second kernel joins the parts.
 #include "paged.h"
 
+#include <algorithm>
+#include <type_traits>
+
 namespace {
 
 constexpr float LOG2E = 1.44269504f;
@@ -65,6 +68,9 @@ struct AttnLaunch {
   int chunk;
   float* ws;   // splits > 1: [slots][Hkv][splits] x ([BM][D] sums, [BM][2] reference and l)
 };
+
+template <int V>
+using Parity = std::integral_constant<int, V>;  // which of the two buffers
 
 template <int WM>
 struct Shape {
@@ -259,21 +265,28 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
   float ref = -INFINITY, l = 0.f;
 
-  // LDS addresses inside a tile: K rows by chunk step, V by (dimension block, key half)
-  const uint32_t k_row = c * D * 2, k_swz = (h ^ swz<D>(c)) << 4;
+  // LDS addresses of a ring, K rows by chunk step and V by (dimension block, key half); the tile's
+  // buffer and its rows are constant offsets
+  const uint32_t k_swz = (h ^ swz<D>(c)) << 4;
   const int v_r = 4 * h + ((lane & 15) >> 2);
-  const uint32_t v_row = v_r * D * 2 + 8 * (lane & 1);
   const uint32_t v_swz = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz<D>(v_r)) << 4;
-  const auto read_v = [&](uint32_t base, int t, int db) {
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        LDS_PTR(s16x4, base + v_row + (v_swz ^ (db << 6)) + t * 16 * D * 2));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        LDS_PTR(s16x4, base + v_row + (v_swz ^ (db << 6) ^ 32) + (t * 16 + 8) * D * 2));
+  uint32_t k_at[D / 16], v_at[D / 32][2];
+#pragma unroll
+  for (int st = 0; st < D / 16; ++st) k_at[st] = k_ring + c * D * 2 + (k_swz ^ (st << 5));
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      v_at[db][u] = k_ring + v_r * D * 2 + 8 * (lane & 1) + (v_swz ^ (db << 6) ^ (u << 5));
+  const auto read_v = [&](auto buf, int t, int db) {
+    constexpr int AT = 2 * TILE + decltype(buf)::value * TILE;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, v_at[db][0]) + (AT + t * 16 * D * 2) / 8);
+    const s16x4 hi =
+        __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, v_at[db][1]) + (AT + (t * 16 + 8) * D * 2) / 8);
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(vec8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  const auto scores = [&](int it, f32x16 (&x)[NB]) {
-    const uint32_t base = k_ring + (it & 1) * TILE + k_row;
+  const auto scores = [&](auto buf, f32x16 (&x)[NB]) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -282,14 +295,14 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     for (int st = 0; st < D / 16; ++st)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        const u32x4 kf = *LDS_PTR(u32x4, base + (k_swz ^ (st << 5)) + nb * 32 * D * 2);
+        const u32x4 kf = LDS_PTR(u32x4, k_at[st])[(decltype(buf)::value * TILE + nb * 32 * D * 2) / 16];
         x[nb] = N::mfma(__builtin_bit_cast(vec8, kf), qf[st], x[nb]);
       }
   };
 
   // Pipeline: iteration i multiplies K of tile i + 1 while it takes the exponentials of tile i,
   // then V of tile i; the copies of K of tile i + 2 and V of tile i + 1 are in flight meanwhile.
-  f32x16 x[NB];
+  f32x16 xa[NB], xb[NB];
   uint32_t have = 0;
   int ids1 = -1, ids2 = -1;  // pages of tiles it + 1 and it + 2
   if (iters > 0) {
@@ -302,9 +315,10 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     ids2 = page_of(2);
     wait_loads();
     if constexpr (WM > 1) lds_barrier();
-    scores(0, x);
+    scores(Parity<0>{}, xa);
   }
-  for (int it = 0; it < iters; ++it) {
+  // x: the tile's scores; xn: the next one's
+  const auto step = [&](auto even, auto odd, int it, f32x16 (&x)[NB], f32x16 (&xn)[NB]) {
     wait_loads();
     if (hides(it, have)) make_finite(it);
     if constexpr (WM > 1)
@@ -355,8 +369,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
       ref = next;
     }
     const float r = ref == -INFINITY ? 0.f : ref;  // no key seen so far
-    f32x16 xn[NB];
-    scores(it + 1, xn);  // past the last tile: of what the buffer holds, not used
+    scores(odd, xn);  // past the last tile: of what the buffer holds, not used
     vec8 pf[2 * NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -366,14 +379,15 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
         l += p;
         pf[2 * nb + i / 8][i % 8] = (T)p;
       }
-    const uint32_t vb = v_ring + (it & 1) * TILE;
 #pragma unroll
     for (int tt = 0; tt < 2 * NB; ++tt)
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) o[db] = N::mfma(read_v(vb, tt, db), pf[tt], o[db]);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) x[nb] = xn[nb];
+      for (int db = 0; db < D / 32; ++db) o[db] = N::mfma(read_v(even, tt, db), pf[tt], o[db]);
     have = have_next;
+  };
+  for (int it = 0; it < iters; it += 2) {
+    step(Parity<0>{}, Parity<1>{}, it, xa, xb);
+    if (it + 1 < iters) step(Parity<1>{}, Parity<0>{}, it + 1, xb, xa);
   }
   l = sum_halves(l);
   __syncthreads();  // put_back is known
@@ -497,11 +511,19 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   }
 }
 
-// Joins the parts of split rows: one wavefront per (row, query head).
-template <typename T, int D>
-__global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, AttnLaunch L, int bm) {
-  const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// Joins the parts of split rows: W wavefronts per (row, query head), D / 4 lanes per part, so
+// that 64 / (D / 4) parts are read at a time and wavefront; four such reads are in flight.
+struct JoinArgs {
+  AttnLaunch l[2];
+  int wm[2], n;
+};
+template <typename T, int D, int W>
+__global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArgs j) {
+  constexpr int LP = D / 4, AT_ONCE = 64 / LP, UNROLL = 4;
+  __shared__ f32x4 so[W > 1 ? W : 1][LP];
+  __shared__ float sl[W > 1 ? W : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t item = W > 1 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   const int row = (int)(item / a.heads), head = (int)(item % a.heads);
   if (row >= a.batch.rows) return;
   const int s = seq_of_row(a.batch.q_start, a.batch.n_seq, row);
@@ -509,49 +531,100 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, AttnLau
   if (!read_seq(a, s, q) || row >= q.start + q.n) return;
   const int Hkv = a.pages.kv_heads, G = a.heads / Hkv, kvh = head / G;
   const int64_t M = (int64_t)q.n * G;
+  const int which = j.n > 1 && !(M > j.l[0].m_lo && M <= j.l[0].m_hi);
+  const AttnLaunch& L = j.l[which];
+  const int bm = 32 * j.wm[which];
   if (M <= L.m_lo || M > L.m_hi) return;
   const int m = (row - q.start) * G + head % G, tile = m / bm, c = m % bm;
-  const int m1 = (int)(M < (tile + 1) * bm ? M : (tile + 1) * bm);
+  const int m1 = (int)(M < (int64_t)(tile + 1) * bm ? M : (int64_t)(tile + 1) * bm);
   const int lim = key_limit(q.len - q.n + (m1 - 1) / G, a.block, q.len);
   if (lim <= L.chunk) return;  // written by its only workgroup
   const int parts = (lim + L.chunk - 1) / L.chunk;
   const int slot = bm == 32 ? s : (int)((int64_t)q.start * G / bm + s) + tile;
-  const float* p0 = L.ws + ((int64_t)slot * Hkv + kvh) * L.splits * part_floats<D>(bm);
+  const int64_t stride = part_floats<D>(bm);
+  const float* const p0 = L.ws + ((int64_t)slot * Hkv + kvh) * L.splits * stride;
+  const float* const refs = p0 + bm * D + 2 * c;
   float top = -INFINITY;
-  for (int k = lane; k < parts; k += 64)
-    top = fmaxf(top, p0[(int64_t)k * part_floats<D>(bm) + bm * D + 2 * c]);
-  top = wave_max(top);
-  float sum = 0.f, acc[D / 64] = {};
-  for (int k = 0; k < parts; ++k) {
-    const float* p = p0 + (int64_t)k * part_floats<D>(bm);
-    const float r = p[bm * D + 2 * c], f = r == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r - top);
-    sum += f * p[bm * D + 2 * c + 1];
-    for (int e = 0; e < D / 64; ++e) acc[e] += f * p[c * D + lane * (D / 64) + e];
+  for (int k = lane; k < parts; k += 64) top = fmaxf(top, refs[k * stride]);
+  const int sub = lane % LP, first = (W > 1 ? wave * AT_ONCE : 0) + lane / LP;
+  constexpr int STEP = AT_ONCE * W;
+  f32x4 acc = {};
+  float sum = 0.f;
+  for (int base = 0; base < parts; base += STEP * UNROLL) {  // the same for all lanes
+    f32x4 v[UNROLL];
+    float r[UNROLL], l[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int k = min(base + first + u * STEP, parts - 1);
+      v[u] = *(const f32x4*)(p0 + k * stride + c * D + 4 * sub);
+      r[u] = refs[k * stride], l[u] = refs[k * stride + 1];
+    }
+    if (base == 0) top = wave_max(top);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      // a part without keys has nothing but zeros (or a NaN that stays)
+      const float f = base + first + u * STEP >= parts ? 0.f : r[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r[u] - top);
+      if (f == 0.f) continue;
+      sum += f * l[u];
+      for (int e = 0; e < 4; ++e) acc[e] += f * v[u][e];
+    }
+  }
+  for (int o = LP; o < 64; o *= 2) {
+    sum += __shfl_xor(sum, o);
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], o);
+  }
+  if constexpr (W > 1) {
+    if (lane < LP) so[wave][lane] = acc;
+    if (lane == 0) sl[wave] = sum;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < W; ++w) {
+      sum += sl[w];
+      for (int e = 0; e < 4; ++e) acc[e] += so[w][sub][e];
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  T* op = (T*)a.out + row * a.ld_out + head * D + lane * (D / 64);
-  for (int e = 0; e < D / 64; ++e) op[e] = (T)(sum == 0.f ? 0.f : acc[e] * inv);
+  if (lane < LP) {
+    typedef T vec4 __attribute__((ext_vector_type(4)));
+    vec4 w;
+    for (int e = 0; e < 4; ++e) w[e] = (T)(sum == 0.f ? 0.f : acc[e] * inv);
+    *(vec4*)((T*)a.out + row * a.ld_out + head * D + 4 * sub) = w;
+  }
   if (a.lse && lane == 0)
     a.lse[(int64_t)row * a.heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// One launch's place in the plan: `tiles` row tiles are expected, `occ` workgroups fit a CU.
+// One launch's place in the plan: `tiles` row tiles are expected. The keys are split where
+// that ends sooner by an estimate in us: a workgroup's iteration (step keys) takes t0 alone (0.75
+// at 64 keys by 128 rows, 1 where the wavefronts take 128 keys), or what the running workgroups'
+// copies take at 5.3 TB/s together; workgroups run in rounds of 256 occ; joining takes 4.5 and
+// the parts' way to memory and back at 4 TB/s. (8 branches of 32 rows over 544 keys, 64
+// workgroups unsplit: 13 us; in 5 parts 15.3 and 7.5 for the joining.)
 PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, int64_t slots, int64_t tiles, int kv_heads, int d,
                      int max_len) {
   const int bm = 32 * wm, step = wm == 1 ? 4 * 32 : (4 / wm) * 64;
   const int occ = (wm == 4 ? 2 : 1) * (d == 64 ? 2 : 1);
-  const int64_t want = 256 * occ, items = tiles * kv_heads;
-  int64_t splits = items > 0 ? want / items : 1;
-  const int64_t most = ceil_div(max_len, 2 * step);
-  splits = splits > most ? most : splits;
-  splits = splits < 1 ? 1 : splits;
-  const int64_t chunk = ceil_div(ceil_div(max_len, splits), step) * step;
-  splits = chunk > 0 ? ceil_div(max_len, chunk) : 1;
+  const double t0 = wm == 1 ? 2.0 : 0.9;
+  const int64_t cus = 256 * occ, items = std::max<int64_t>(1, tiles * kv_heads);
+  const int64_t most = std::max<int64_t>(1, ceil_div(max_len, step));
+  double least = 1e30;
+  int64_t splits = 1;
+  for (int64_t s = 1; s <= most && s <= 1024; s = s < 4 ? s + 1 : s * 4 / 3) {
+    const int64_t iters = ceil_div(ceil_div(max_len, s), step);
+    const double load = (double)items * s / cus, rounds = load <= 1.0 ? 1.0 : load + 0.5;
+    const double running = (double)std::min(items * s, cus);
+    const double t_it = wm == 1 ? std::max(t0, running * step * d * 4 / 5.3e6) : t0;
+    double t = rounds * iters * t_it;
+    if (s > 1) t += 4.5 + items * s * bm * d * 8 / 4e6;
+    if (t < least) least = t, splits = s;
+  }
+  const int64_t chunk = std::max<int64_t>(1, ceil_div(ceil_div(max_len, splits), step)) * step;
+  splits = std::max<int64_t>(1, ceil_div(max_len, chunk));
   PagedPlan::Part p{};
   p.wm = wm, p.m_lo = m_lo, p.m_hi = m_hi;
-  p.slots = slots, p.splits = (int)splits, p.chunk = (int)(chunk > 0 ? chunk : step);
+  p.slots = slots, p.splits = (int)splits, p.chunk = (int)chunk;
   p.ws_bytes = splits > 1 ? slots * kv_heads * splits * (int64_t)bm * (d + 2) * 4 : 0;
   return p;
 }
@@ -576,6 +649,8 @@ hipError_t launch(const PagedAttnArgs& a, const AttnLaunch& L, hipStream_t s) {
 template <typename T, int D>
 hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t s) {
   char* ws = (char*)a.ws;
+  JoinArgs j{};
+  int most = 0;
   for (int i = 0; i < plan.n; ++i) {
     const PagedPlan::Part& p = plan.part[i];
     const AttnLaunch L{p.m_lo, p.m_hi, (int)p.slots, p.splits, p.chunk, (float*)ws};
@@ -590,11 +665,18 @@ hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
       e = cap ? launch<T, D, 4, true>(a, L, s) : launch<T, D, 4, false>(a, L, s);
     if (e != hipSuccess) return e;
     if (p.splits > 1) {
-      const int64_t n = ceil_div((int64_t)a.batch.rows * a.heads, 4);
-      attn_join_kernel<T, D><<<dim3((unsigned)n), dim3(256), 0, s>>>(a, L, 32 * p.wm);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
+      j.l[j.n] = L, j.wm[j.n++] = p.wm;
+      most = p.splits > most ? p.splits : most;
     }
+  }
+  if (j.n) {
+    // many parts: a workgroup per (row, query head)
+    const int64_t items = (int64_t)a.batch.rows * a.heads;
+    if (most > 16)
+      attn_join_kernel<T, D, 4><<<dim3((unsigned)items), dim3(256), 0, s>>>(a, j);
+    else
+      attn_join_kernel<T, D, 1><<<dim3((unsigned)ceil_div(items, 4)), dim3(256), 0, s>>>(a, j);
+    return hipGetLastError();
   }
   return hipSuccess;
 }

@@ -108,6 +108,17 @@ def test_attention_long(lp, n, m, d):
     check_attend(lp, b, q, 1)
 
 
+@pytest.mark.parametrize("m", [500, 700, 1000, 1500, 3000, 70000])
+@pytest.mark.parametrize("heads,kv_heads,d", [(8, 2, 64), (28, 4, 128), (1, 1, 64)])
+def test_attention_parts(lp, m, heads, kv_heads, d):
+    """One token whose keys are split over few and many workgroups, with scores far below zero
+    (a joined part's reference is not near 0)."""
+    b = ref.Batch([(1, m), (1, m // 2)], 64, kv_heads, d, BF, m, fill=math.nan)
+    q = randn(6, (2, heads, d), BF, 2.0)
+    b.k = torch.where(torch.isnan(b.k), b.k, b.k * 0.2 - 1.0 * q[0, 0].sign() * (heads == 1))
+    check_attend(lp, b, q, 1)
+
+
 def test_attention_peaked(lp):
     """The largest score comes first, last or in the middle, far above the rest."""
     b = ref.Batch([(1, 900), (40, 900)], 64, 2, 128, BF, 2)
