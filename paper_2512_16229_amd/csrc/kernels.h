@@ -206,6 +206,7 @@ struct AppendArgs {
   const void *q_norm, *k_norm;  // null: no norm
   float eps;
   int rotate;
+  int page_shift;  // page_size = 1 << page_shift
   double turns[64];  // turns per position of pair j < head_dim / 2
 };
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);

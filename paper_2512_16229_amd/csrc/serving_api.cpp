@@ -111,6 +111,7 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
   a.q_norm = q_norm, a.k_norm = k_norm;
   a.eps = eps;
   a.rotate = rope_theta > 0.f;
+  a.page_shift = __builtin_ctz(pages->page_size);
   // turns per position of each pair, in fp64
   for (int j = 0; j < d / 2; ++j)
     a.turns[j] = a.rotate ? std::pow((double)rope_theta, -2.0 * j / d) / (2.0 * M_PI) : 0.0;
