@@ -276,12 +276,12 @@ _DTYPES = {torch.bfloat16: LOPA_BF16, torch.float16: LOPA_F16, torch.float32: LO
 
 
 def _on(t, name):
-    """The device of a call: that of its first tensor."""
+    """The device (its index) of a call: that of its first tensor."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
     if not t.is_cuda:
         raise ValueError(f"{name}: must be a device tensor")
-    return t.device
+    return t.get_device()
 
 
 def _arg(t, dtype, dev, name, shape=None):
@@ -290,9 +290,9 @@ def _arg(t, dtype, dev, name, shape=None):
         return None
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
-    if t.device != dev:
-        raise ValueError(f"{name}: must be a device tensor on {dev}")
-    if dtype is not None and t.dtype != dtype:
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: must be a device tensor on cuda:{dev}")
+    if dtype is not None and t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
@@ -305,9 +305,9 @@ def _rows_arg(t, dtype, dev, name, shape):
     """Address and row stride of a [rows][heads][head_dim] tensor with contiguous heads."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor")
-    if t.device != dev:
-        raise ValueError(f"{name}: must be a device tensor on {dev}")
-    if t.dtype != dtype:
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: must be a device tensor on cuda:{dev}")
+    if t.dtype is not dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {shape}, got {tuple(t.shape)}")
@@ -321,16 +321,18 @@ def _rows_arg(t, dtype, dev, name, shape):
 def _call(f, dev, stream, *args):
     """f(*args, stream) on the device that holds the arrays, on its current stream or the given one."""
     if stream is None:
-        st = torch.cuda.current_stream(dev).cuda_stream
+        st = torch._C._cuda_getCurrentRawStream(dev)  # current_stream(dev).cuda_stream without its object
     else:
-        if hasattr(stream, "device") and stream.device != dev:
-            raise ValueError(f"stream of {stream.device}, the tensors on {dev}")
+        if hasattr(stream, "device") and stream.device.index != dev:
+            raise ValueError(f"stream of {stream.device}, the tensors on cuda:{dev}")
         st = _stream(stream)
-    if torch.cuda.current_device() == dev.index:
-        _check(f(*args, st))
+    if torch.cuda.current_device() == dev:
+        status = f(*args, st)
     else:
         with torch.cuda.device(dev):
-            _check(f(*args, st))
+            status = f(*args, st)
+    if status:
+        _check(status)
 
 
 def _paged(k_pages, v_pages, table, q_start, kv_len, rows, dev):

@@ -112,9 +112,10 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
   a.eps = eps;
   a.rotate = rope_theta > 0.f;
   a.page_shift = __builtin_ctz(pages->page_size);
-  // turns per position of each pair, in fp64
-  for (int j = 0; j < d / 2; ++j)
-    a.turns[j] = a.rotate ? std::pow((double)rope_theta, -2.0 * j / d) / (2.0 * M_PI) : 0.0;
+  // turns per position of each pair, in fp64 (one product a pair: off by j 2^-53)
+  const double ratio = a.rotate ? std::pow((double)rope_theta, -2.0 / d) : 0.0;
+  double turns = a.rotate ? 1.0 / (2.0 * M_PI) : 0.0;
+  for (int j = 0; j < d / 2; ++j, turns *= ratio) a.turns[j] = turns;
   return launched(launch_paged_append(a, (hipStream_t)stream), "paged append");
 }
 
