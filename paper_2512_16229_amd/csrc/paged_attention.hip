@@ -60,9 +60,25 @@ struct Num<_Float16> {
   }
 };
 
+// n / d for 32-bit n by two products, with m = ceil(2^64 / d) from the host (0 for d = 1): the
+// error n (m d - 2^64) / (2^64 d) stays below 1 / d. A kernel of few keys is bound by the
+// instructions on its way to them, and a division is about forty.
+struct Div {
+  uint32_t d;
+  uint32_t hi, lo;
+};
+Div divider(uint32_t d) {
+  const uint64_t m = d > 1 ? UINT64_MAX / d + 1 : 0;
+  return {d, (uint32_t)(m >> 32), (uint32_t)m};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Div& v) {
+  return v.d == 1 ? n : (uint32_t)(((uint64_t)n * v.hi + (((uint64_t)n * v.lo) >> 32)) >> 32);
+}
+
 // A launch covers the sequences with m_lo < rows x G <= m_hi.
 struct AttnLaunch {
   int64_t m_lo, m_hi;
+  Div group, kv_heads, per_split, block;  // heads / kv_heads; kv_heads; splits; the mask's block
   int slots;   // row tiles' places: tile t of sequence s at floor(q_start[s] G / BM) + s + t
   int splits;  // key splits of `chunk` keys
   int chunk;
@@ -82,10 +98,10 @@ template <int D>
 constexpr int part_floats(int bm) { return bm * (D + 2); }
 
 // position limit: keys at or past it are hidden from a row at position p
-__device__ __forceinline__ int key_limit(int p, int block, int len) {
-  if (block == 0) return len;
+__device__ __forceinline__ int key_limit(int p, const Div& block, int len) {
+  if (block.d == 0) return len;
   if (p < 0) return 0;
-  const int64_t lim = ((int64_t)(p / block) + 1) * block;
+  const int64_t lim = ((int64_t)quotient(p, block) + 1) * block.d;
   return lim < len ? (int)lim : len;
 }
 
@@ -139,9 +155,9 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave % WM, wk = wave / WM;
-  const int Hkv = a.pages.kv_heads, G = a.heads / Hkv, ps = a.pages.page_size;
-  const int kvh = blockIdx.x % Hkv, rest = blockIdx.x / Hkv;
-  const int split = rest % L.splits, slot = L.slots - 1 - rest / L.splits;
+  const int Hkv = a.pages.kv_heads, G = L.group.d, ps = a.pages.page_size;
+  const int rest = quotient(blockIdx.x, L.kv_heads), kvh = blockIdx.x - rest * Hkv;
+  const int back = quotient(rest, L.per_split), split = rest - back * L.splits, slot = L.slots - 1 - back;
 
   // which sequence and row tile
   int s, tile = 0;
@@ -163,7 +179,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   if (M <= L.m_lo || M > L.m_hi || (int64_t)tile * BM >= M) return;
   const int m0 = tile * BM, m1 = (int)(M < m0 + BM ? M : m0 + BM);  // this tile's rows
   const int pos0 = q.len - q.n;
-  const int lim_tile = key_limit(pos0 + (m1 - 1) / G, a.block, q.len);
+  const int lim_tile = key_limit(pos0 + (int)quotient(m1 - 1, L.group), L.block, q.len);
   const int k0 = split * L.chunk;
   if (split > 0 && k0 >= lim_tile) return;
   const int k1 = lim_tile < k0 + L.chunk ? lim_tile : k0 + L.chunk;
@@ -172,11 +188,11 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   const int c = lane & 31, h = lane >> 5;
   const int w0 = m0 + 32 * wm;  // the wavefront's first row
   const int m = w0 + c < m1 ? w0 + c : m1 - 1;
-  const int row = q.start + m / G, head = kvh * G + m % G;
-  const int lim = key_limit(pos0 + m / G, a.block, q.len);
-  const bool idle = w0 >= m1;
-  const int lim_min = idle ? 0 : key_limit(pos0 + w0 / G, a.block, q.len);
-  const int lim_max = idle ? 0 : key_limit(pos0 + ((w0 + 31 < m1 ? w0 + 31 : m1 - 1)) / G, a.block, q.len);
+  const int mr = quotient(m, L.group), row = q.start + mr, head = kvh * G + m - mr * G;
+  const int lim = key_limit(pos0 + mr, L.block, q.len);
+  // rows are in order, and so are their limits
+  const int lim_min = w0 < m1 ? __builtin_amdgcn_readlane(lim, 0) : 0;
+  const int lim_max = w0 < m1 ? __builtin_amdgcn_readlane(lim, 31) : 0;
 
   // scores in units of log2: x = sc (q . K), the sign of the scale in q; a scale of 0 is q = 0
   const float sc = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
@@ -228,7 +244,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   // A value of V that is not finite would reach rows that do not see its key as 0 x infinity.
   // Where a tile hides keys from some row of the workgroup such values are taken as zeros, by
   // the wavefront that copied them, and put back after the loop for the rows that see them.
-  const int lim_first = key_limit(pos0 + m0 / G, a.block, q.len);  // of the tile's first row
+  const int lim_first = key_limit(pos0 + (int)quotient(m0, L.group), L.block, q.len);  // of the tile's first row
   const auto hides = [&](int it, uint32_t have) {
     return have != ALL || (first + it * WK + 1) * KT > lim_first;
   };
@@ -487,18 +503,18 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
           for (int u = 0; u < 4; ++u) acc[e + u] += rk == -INFINITY ? v[u] : f[k] * v[u];
         }
       }
-      const int mm = m0 + rr;
+      const int mm = m0 + rr, mq = quotient(mm, L.group);
       if (whole) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int64_t r2 = q.start + mm / G;
-        T* op = out + r2 * a.ld_out + (kvh * G + mm % G) * D + e0;
+        const int64_t r2 = q.start + mq;
+        T* op = out + r2 * a.ld_out + (kvh * G + mm - mq * G) * D + e0;
         for (int e = 0; e < E; e += 8) {
           vec8 w;
           for (int u = 0; u < 8; ++u) w[u] = (T)(sum == 0.f ? 0.f : acc[e + u] * inv);
           *(vec8*)(op + e) = w;
         }
         if (a.lse && e0 == 0)
-          a.lse[r2 * a.heads + kvh * G + mm % G] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * ln2;
+          a.lse[r2 * a.heads + kvh * G + mm - mq * G] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * ln2;
       } else {
         for (int e = 0; e < E; e += 4)
           *(f32x4*)(part + rr * D + e0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
@@ -523,24 +539,23 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
   __shared__ f32x4 so[W > 1 ? W : 1][LP];
   __shared__ float sl[W > 1 ? W : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t item = W > 1 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  const int row = (int)(item / a.heads), head = (int)(item % a.heads);
-  if (row >= a.batch.rows) return;
+  const int row = blockIdx.x, head = W > 1 ? blockIdx.y : blockIdx.y * 4 + wave;
+  if (head >= a.heads) return;
   const int s = seq_of_row(a.batch.q_start, a.batch.n_seq, row);
   Seq q;
   if (!read_seq(a, s, q) || row >= q.start + q.n) return;
-  const int Hkv = a.pages.kv_heads, G = a.heads / Hkv, kvh = head / G;
+  const int Hkv = a.pages.kv_heads, G = j.l[0].group.d, kvh = quotient(head, j.l[0].group);
   const int64_t M = (int64_t)q.n * G;
   const int which = j.n > 1 && !(M > j.l[0].m_lo && M <= j.l[0].m_hi);
   const AttnLaunch& L = j.l[which];
-  const int bm = 32 * j.wm[which];
+  const int lb = 5 + j.wm[which] / 2, bm = 1 << lb;  // 32, 64 or 128 rows
   if (M <= L.m_lo || M > L.m_hi) return;
-  const int m = (row - q.start) * G + head % G, tile = m / bm, c = m % bm;
+  const int m = (row - q.start) * G + head - kvh * G, tile = m >> lb, c = m & (bm - 1);
   const int m1 = (int)(M < (int64_t)(tile + 1) * bm ? M : (int64_t)(tile + 1) * bm);
-  const int lim = key_limit(q.len - q.n + (m1 - 1) / G, a.block, q.len);
+  const int lim = key_limit(q.len - q.n + (int)quotient(m1 - 1, L.group), L.block, q.len);
   if (lim <= L.chunk) return;  // written by its only workgroup
   const int parts = (lim + L.chunk - 1) / L.chunk;
-  const int slot = bm == 32 ? s : (int)((int64_t)q.start * G / bm + s) + tile;
+  const int slot = bm == 32 ? s : (int)(((int64_t)q.start * G >> lb) + s) + tile;
   const int64_t stride = part_floats<D>(bm);
   const float* const p0 = L.ws + ((int64_t)slot * Hkv + kvh) * L.splits * stride;
   const float* const refs = p0 + bm * D + 2 * c;
@@ -653,7 +668,8 @@ hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
   int most = 0;
   for (int i = 0; i < plan.n; ++i) {
     const PagedPlan::Part& p = plan.part[i];
-    const AttnLaunch L{p.m_lo, p.m_hi, (int)p.slots, p.splits, p.chunk, (float*)ws};
+    const AttnLaunch L{p.m_lo, p.m_hi, divider(a.heads / a.pages.kv_heads), divider(a.pages.kv_heads),
+                       divider(p.splits), divider(a.block), (int)p.slots, p.splits, p.chunk, (float*)ws};
     ws += p.ws_bytes;
     const bool cap = a.softcap > 0.f;
     hipError_t e;
@@ -671,11 +687,10 @@ hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
   }
   if (j.n) {
     // many parts: a workgroup per (row, query head)
-    const int64_t items = (int64_t)a.batch.rows * a.heads;
     if (most > 16)
-      attn_join_kernel<T, D, 4><<<dim3((unsigned)items), dim3(256), 0, s>>>(a, j);
+      attn_join_kernel<T, D, 4><<<dim3(a.batch.rows, a.heads), dim3(256), 0, s>>>(a, j);
     else
-      attn_join_kernel<T, D, 1><<<dim3((unsigned)ceil_div(items, 4)), dim3(256), 0, s>>>(a, j);
+      attn_join_kernel<T, D, 1><<<dim3(a.batch.rows, (a.heads + 3) / 4), dim3(256), 0, s>>>(a, j);
     return hipGetLastError();
   }
   return hipSuccess;
