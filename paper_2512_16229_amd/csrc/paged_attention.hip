@@ -612,16 +612,15 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // One launch's place in the plan: `tiles` row tiles are expected. The keys are split where
-// that ends sooner by an estimate in us: a workgroup's iteration (step keys) takes t0 alone (0.75
-// at 64 keys by 128 rows, 1 where the wavefronts take 128 keys), or what the running workgroups'
-// copies take at 5.3 TB/s together; workgroups run in rounds of 256 occ; joining takes 4.5 and
-// the parts' way to memory and back at 4 TB/s. (8 branches of 32 rows over 544 keys, 64
-// workgroups unsplit: 13 us; in 5 parts 15.3 and 7.5 for the joining.)
+// that ends sooner by an estimate in us: a workgroup's iteration (step keys) takes 0.9 at 64 keys
+// by 128 rows; where the wavefronts take 128 keys 1.2 and the running workgroups' share of 8 TB/s
+// (one token over 131072 keys and 8 K / V heads: 158 us of 13 parts, 114 of 22, 102 of 32);
+// workgroups run in rounds of 256 occ; joining takes 4.5 and the parts' way to memory and back at
+// 4 TB/s (8 branches of 32 rows over 544 keys: 21 us unsplit, 15 and 7.5 for joining in 5 parts).
 PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, int64_t slots, int64_t tiles, int kv_heads, int d,
                      int max_len) {
   const int bm = 32 * wm, step = wm == 1 ? 4 * 32 : (4 / wm) * 64;
   const int occ = (wm == 4 ? 2 : 1) * (d == 64 ? 2 : 1);
-  const double t0 = wm == 1 ? 2.0 : 0.9;
   const int64_t cus = 256 * occ, items = std::max<int64_t>(1, tiles * kv_heads);
   const int64_t most = std::max<int64_t>(1, ceil_div(max_len, step));
   double least = 1e30;
@@ -630,7 +629,7 @@ PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, int64_t slots, int64_t 
     const int64_t iters = ceil_div(ceil_div(max_len, s), step);
     const double load = (double)items * s / cus, rounds = load <= 1.0 ? 1.0 : load + 0.5;
     const double running = (double)std::min(items * s, cus);
-    const double t_it = wm == 1 ? std::max(t0, running * step * d * 4 / 5.3e6) : t0;
+    const double t_it = wm == 1 ? 1.2 + running * step * d * 4 / 8e6 : 0.9;
     double t = rounds * iters * t_it;
     if (s > 1) t += 4.5 + items * s * bm * d * 8 / 4e6;
     if (t < least) least = t, splits = s;
