@@ -215,9 +215,11 @@ struct PagedPlan {
   struct Part {           // one launch: the sequences with m_lo < rows x group <= m_hi
     int wm;               // 32 wm rows a workgroup
     int64_t m_lo, m_hi;
+    bool single;          // no sequence has more than one row tile
     int64_t slots;        // row tiles' places
     int splits, chunk;    // key splits of `chunk` keys
     int64_t ws_bytes;
+    double us;            // expected
   } part[2];
   int n;
   int64_t bytes;  // workspace of all parts

@@ -79,7 +79,8 @@ __device__ __forceinline__ uint32_t quotient(uint32_t n, const Div& v) {
 struct AttnLaunch {
   int64_t m_lo, m_hi;
   Div group, kv_heads, per_split, block;  // heads / kv_heads; kv_heads; splits; the mask's block
-  int slots;   // row tiles' places: tile t of sequence s at floor(q_start[s] G / BM) + s + t
+  int slots;   // row tiles' places: tile t of sequence s at floor(q_start[s] G / BM) + s + t,
+  int single;  // or at s where no sequence has more than one
   int splits;  // key splits of `chunk` keys
   int chunk;
   float* ws;   // splits > 1: [slots][Hkv][splits] x ([BM][D] sums, [BM][2] reference and l)
@@ -160,10 +161,8 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   const int back = quotient(rest, L.per_split), split = rest - back * L.splits, slot = L.slots - 1 - back;
 
   // which sequence and row tile
-  int s, tile = 0;
-  if constexpr (WM == 1) {
-    s = slot;
-  } else {
+  int s = slot, tile = 0;
+  if (!L.single) {
     int n = 0;
     for (int base = 0; base < a.batch.n_seq; base += 64) {
       const int i = base + lane;
@@ -174,7 +173,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   }
   Seq q;
   if (!read_seq(a, s, q)) return;
-  if constexpr (WM != 1) tile = slot - (int)((int64_t)q.start * G / BM + s);
+  if (!L.single) tile = slot - (int)((int64_t)q.start * G / BM + s);
   const int64_t M = (int64_t)q.n * G;
   if (M <= L.m_lo || M > L.m_hi || (int64_t)tile * BM >= M) return;
   const int m0 = tile * BM, m1 = (int)(M < m0 + BM ? M : m0 + BM);  // this tile's rows
@@ -555,7 +554,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
   const int lim = key_limit(q.len - q.n + (int)quotient(m1 - 1, L.group), L.block, q.len);
   if (lim <= L.chunk) return;  // written by its only workgroup
   const int parts = (lim + L.chunk - 1) / L.chunk;
-  const int slot = bm == 32 ? s : (int)(((int64_t)q.start * G >> lb) + s) + tile;
+  const int slot = L.single ? s : (int)(((int64_t)q.start * G >> lb) + s) + tile;
   const int64_t stride = part_floats<D>(bm);
   const float* const p0 = L.ws + ((int64_t)slot * Hkv + kvh) * L.splits * stride;
   const float* const refs = p0 + bm * D + 2 * c;
@@ -611,35 +610,41 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// One launch's place in the plan: `tiles` row tiles are expected. The keys are split where
-// that ends sooner by an estimate in us: a workgroup's iteration (step keys) takes 0.9 at 64 keys
-// by 128 rows; where the wavefronts take 128 keys 1.2 and the running workgroups' share of 8 TB/s
-// (one token over 131072 keys and 8 K / V heads: 158 us of 13 parts, 114 of 22, 102 of 32);
-// workgroups run in rounds of 256 occ; joining takes 4.5 and the parts' way to memory and back at
-// 4 TB/s (8 branches of 32 rows over 544 keys: 21 us unsplit, 15 and 7.5 for joining in 5 parts).
-PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, int64_t slots, int64_t tiles, int kv_heads, int d,
-                     int max_len) {
-  const int bm = 32 * wm, step = wm == 1 ? 4 * 32 : (4 / wm) * 64;
+// One launch's place in the plan, and what it is expected to take in us. `tiles` row tiles of
+// `seqs` sequences. The keys are split where that ends sooner:
+//   an iteration of a workgroup is 128 keys by 32 rows (wm = 1), 128 by 64 (2) or 64 by 128 (4);
+//   at head_dim 128 it takes 1.55 where a wavefront has 64 keys (2.13 for each of two workgroups
+//   on a CU), 1.2 where it has 32, and the running sequences' share of 8 TB/s on top of that
+//   where all keys come from memory (one token over 131072 keys and 8 K / V heads: 158 us in 13
+//   parts, 114 in 22, 102 in 32);
+//   workgroups run in rounds of 256 occ;
+//   joining takes 4.5 and the parts' way to memory and back at 4 TB/s (8 branches of 32 rows over
+//   544 keys, wm = 4: 21 unsplit, 15 and 7.5 for joining in 5 parts).
+PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, bool single, int64_t slots, int64_t tiles, int64_t seqs,
+                     int kv_heads, int d, int max_len) {
+  const int bm = 32 * wm, step = wm == 4 ? 64 : 128;
   const int occ = (wm == 4 ? 2 : 1) * (d == 64 ? 2 : 1);
-  const int64_t cus = 256 * occ, items = std::max<int64_t>(1, tiles * kv_heads);
+  const double work = d == 64 ? 0.65 : 1.0;
+  const int64_t items = std::max<int64_t>(1, tiles * kv_heads);
   const int64_t most = std::max<int64_t>(1, ceil_div(max_len, step));
   double least = 1e30;
   int64_t splits = 1;
   for (int64_t s = 1; s <= most && s <= 1024; s = s < 4 ? s + 1 : s * 4 / 3) {
-    const int64_t iters = ceil_div(ceil_div(max_len, s), step);
-    const double load = (double)items * s / cus, rounds = load <= 1.0 ? 1.0 : load + 0.5;
-    const double running = (double)std::min(items * s, cus);
-    const double t_it = wm == 1 ? 1.2 + running * step * d * 4 / 8e6 : 0.9;
-    double t = rounds * iters * t_it;
-    if (s > 1) t += 4.5 + items * s * bm * d * 8 / 4e6;
+    const double iters = ceil_div(ceil_div(max_len, s), step), n = (double)items * s;
+    const double load = n / (256 * occ), rounds = load <= 1.0 ? 1.0 : load + 0.5;
+    const double streams = std::min(n, 256.0 * occ) * std::min(1.0, (double)seqs / tiles);
+    double t_it = wm == 1 ? 1.2 * work + streams * step * d * 4 / 8e6 : wm == 4 && n > 256 ? 2.13 * work : 1.55 * work;
+    double t = (wm == 1 ? 0.0 : 2.0) + rounds * iters * t_it;
+    if (s > 1) t += 4.5 + n * bm * d * 8 / 4e6;
     if (t < least) least = t, splits = s;
   }
   const int64_t chunk = std::max<int64_t>(1, ceil_div(ceil_div(max_len, splits), step)) * step;
   splits = std::max<int64_t>(1, ceil_div(max_len, chunk));
   PagedPlan::Part p{};
-  p.wm = wm, p.m_lo = m_lo, p.m_hi = m_hi;
+  p.wm = wm, p.m_lo = m_lo, p.m_hi = m_hi, p.single = single;
   p.slots = slots, p.splits = (int)splits, p.chunk = (int)chunk;
   p.ws_bytes = splits > 1 ? slots * kv_heads * splits * (int64_t)bm * (d + 2) * 4 : 0;
+  p.us = least;
   return p;
 }
 
@@ -668,7 +673,7 @@ hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
   for (int i = 0; i < plan.n; ++i) {
     const PagedPlan::Part& p = plan.part[i];
     const AttnLaunch L{p.m_lo, p.m_hi, divider(a.heads / a.pages.kv_heads), divider(a.pages.kv_heads),
-                       divider(p.splits), divider(a.block), (int)p.slots, p.splits, p.chunk, (float*)ws};
+                       divider(p.splits), divider(a.block), (int)p.slots, p.single, p.splits, p.chunk, (float*)ws};
     ws += p.ws_bytes;
     const bool cap = a.softcap > 0.f;
     hipError_t e;
@@ -697,28 +702,41 @@ hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
 
 }  // namespace
 
+// Rows of a sequence and K / V head up to 32 (a decode step): the wavefronts split the keys.
+// More: 32, 64 or 128 rows a workgroup, whichever is expected to end first - many small ones
+// where they all run at once, large ones where they do not (8 branches of 32 rows, 28 / 4 heads,
+// over 544 keys: 12 us in tiles of 32 rows, 21 in tiles of 128; an 8191-row prompt takes 1.5
+// times as long in tiles of 32). In a batch of unequal sequences tiles of 64 and 128 rows leave
+// those of up to 32 to a launch of their own.
 PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
                                int max_len) {
-  PagedPlan plan{};
-  if (n_seq < 1 || rows < 1 || max_rows < 1) return plan;
+  PagedPlan best{};
+  if (n_seq < 1 || rows < 1 || max_rows < 1) return best;
   if (max_rows > rows) max_rows = rows;
   const int64_t G = heads / kv_heads, most = max_rows * G, all = INT64_MAX;
-  // rows of a sequence and K / V head: up to 32 (a decode step) the wavefronts split the
-  // keys, up to 64 half and half, above that they split the rows
-  const int wm = most <= 32 ? 1 : most <= 64 ? 2 : 4;
   const bool even = rows == (int64_t)n_seq * max_rows;
-  const auto slots = [&](int bm) { return rows * G / bm + n_seq; };
-  if (wm == 1) {
-    plan.part[plan.n++] = part(1, 0, 32, n_seq, n_seq, kv_heads, d, max_len);
-  } else if (even) {
-    plan.part[plan.n++] = part(wm, 0, all, slots(32 * wm), n_seq * ceil_div(most, 32 * wm), kv_heads, d, max_len);
-  } else {
-    // unequal sequences: the short ones in a launch of their own
-    plan.part[plan.n++] = part(wm, 32, all, slots(32 * wm), ceil_div(rows * G, 32 * wm), kv_heads, d, max_len);
-    plan.part[plan.n++] = part(1, 0, 32, n_seq, n_seq, kv_heads, d, max_len);
+  double least = 1e30;
+  for (int wm : {1, 2, 4}) {
+    const int bm = 32 * wm;
+    if (wm > 1 && most <= bm / 2) break;
+    const bool single = most <= bm;
+    const int64_t slots = single ? n_seq : rows * G / bm + n_seq;
+    const int64_t tiles = single ? n_seq : even ? n_seq * ceil_div(most, bm) : ceil_div(rows * G, bm) + n_seq / 2;
+    PagedPlan plan{};
+    double us;
+    if (wm == 1 || even) {
+      plan.part[plan.n++] = part(wm, 0, all, single, slots, tiles, n_seq, kv_heads, d, max_len);
+      us = plan.part[0].us;
+    } else {
+      const int64_t large = std::max<int64_t>(1, std::min<int64_t>(n_seq, rows * G / most));
+      plan.part[plan.n++] = part(wm, 32, all, single, slots, ceil_div(rows * G, bm), large, kv_heads, d, max_len);
+      plan.part[plan.n++] = part(1, 0, 32, true, n_seq, n_seq, n_seq, kv_heads, d, max_len);
+      us = plan.part[0].us + plan.part[1].us + 6.0;
+    }
+    if (us < least) least = us, best = plan;
   }
-  for (int i = 0; i < plan.n; ++i) plan.bytes += plan.part[i].ws_bytes;
-  return plan;
+  for (int i = 0; i < best.n; ++i) best.bytes += best.part[i].ws_bytes;
+  return best;
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedPlan& p, hipStream_t s) {
