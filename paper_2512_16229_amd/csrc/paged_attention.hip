@@ -655,11 +655,6 @@ hipError_t launch(const PagedAttnArgs& a, const AttnLaunch& L, hipStream_t s) {
   constexpr int join = WK == 1 ? 0 : WK * BM * (D + 4 + 2) * 4;
   constexpr int bytes = ring > join ? ring : join;
   static_assert(bytes <= 160 * 1024, "LDS of one CU");
-  if constexpr (bytes > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute((const void*)attn_kernel<T, D, WM, CAP>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-  }
   const int64_t n = (int64_t)L.slots * L.splits * a.pages.kv_heads;
   attn_kernel<T, D, WM, CAP><<<dim3((unsigned)n), dim3(256), bytes, s>>>(a, L);
   return hipGetLastError();

@@ -108,6 +108,55 @@ def test_attention_long(lp, n, m, d):
     check_attend(lp, b, q, 1)
 
 
+# What the launch plan makes of a batch goes by its sizes: these reach the tiles of 64 and of 128
+# rows, whole and with split keys, one and several of a sequence, and two launches in one call.
+VARIANTS = {
+    "64 rows": ([(64, 1000)] * 32, 8, 8, 128),
+    "64 rows, d 64": ([(64, 1000)] * 32, 8, 8, 64),
+    "tiles of 64, split": ([(700, 9000)], 2, 1, 128),
+    "tiles of 64, split, d 64": ([(900, 12000)], 4, 1, 64),
+    "tiles of 128": ([(300, 300)] * 16, 28, 4, 128),
+    "tiles of 128, d 64": ([(300, 300)] * 16, 28, 4, 64),
+    "tiles of 128, split": ([(700, 8300)], 8, 2, 128),
+    "tiles of 128, split, d 64": ([(1500, 9000)], 8, 2, 64),
+    "two launches": ([(1600, 2500)] + [(1, 60 * s + 1) for s in range(38)] + [(2, 2)], 16, 4, 128),
+    "two launches, d 64": ([(1, 55 * s + 1) for s in range(69)] + [(4000, 4000)], 12, 4, 64),
+}
+
+
+@pytest.mark.parametrize("shape", VARIANTS)
+@pytest.mark.parametrize("dtype,page,block,softcap", [(BF, 16, 1, 0.0), (HF, 128, 32, 0.0), (BF, 64, 0, 20.0)])
+def test_attention_variants(lp, shape, dtype, page, block, softcap):
+    lens, heads, kv_heads, d = VARIANTS[shape]
+    b = ref.Batch(lens, page, kv_heads, d, dtype, 31, fill=math.nan)
+    q = randn(7, (b.rows + 2, heads, d), dtype, 1.5)
+    check_attend(lp, b, q, block, softcap)
+
+
+@pytest.mark.parametrize("shape", ["64 rows", "tiles of 64, split", "tiles of 128", "tiles of 128, split, d 64"])
+def test_attention_variants_missing_and_hidden(lp, shape):
+    """Missing pages, and values that are not finite in keys some rows see and some do not."""
+    lens, heads, kv_heads, d = VARIANTS[shape]
+    b = ref.Batch(lens, 32, kv_heads, d, BF, 32)
+    q = randn(7, (b.rows, heads, d), BF)
+    n, m = lens[0]
+    b.table[0, 1] = -1
+    b.table[0, 5] = 10 ** 8
+    clean, clse = check_attend(lp, b, q, 1)
+    at = m - n // 2  # rows of the sequence before n - n // 2 do not see it
+    page, slot = b.table[0, at // 32].long(), at % 32
+    b.v[page, :, slot, 3] = math.inf
+    b.v[page, :, slot, 60] = math.nan
+    out, lse = attend(lp, b, q, 1)
+    k = n - n // 2
+    assert torch.equal(out[:k], clean[:k]) and torch.equal(lse, clse)
+    assert (out[k:n, :, 3] == math.inf).all() and torch.isnan(out[k:n, :, 60]).all()
+    rest = [i for i in range(d) if i not in (3, 60)]
+    # the other values travel with the key's as before
+    ref.close(out[k:n][..., rest], clean[k:n][..., rest], 0.0)
+    assert torch.equal(out[n:], clean[n:])
+
+
 @pytest.mark.parametrize("m", [500, 700, 1000, 1500, 3000, 70000])
 @pytest.mark.parametrize("heads,kv_heads,d", [(8, 2, 64), (28, 4, 128), (1, 1, 64)])
 def test_attention_parts(lp, m, heads, kv_heads, d):
