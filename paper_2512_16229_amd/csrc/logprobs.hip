@@ -19,17 +19,19 @@
 // ranked. (Keeping the n best of each wavefront's stream in the pass itself took 48
 // instead of 30 us at 256 rows of 152064 fp32 logits, n = 20: nearly every segment
 // brings some logit that passes.)
-// Selection works on 64-bit keys that order by (value, lowest index). A wavefront's
-// bound is the n-th largest maximum of groups of lanes (with twice as many groups as n
-// about 1.4 n keys pass it); what passes goes to a buffer in LDS, and a full one is cut
-// to the n best, a key's rank being the number of larger ones.
+// Selection works on 64-bit keys that order by (value, lowest index). A bound that n
+// values reach comes first (of the maxima: the n-th largest maximum of groups of lanes,
+// the largest of the wavefronts'; of the groups' logits: the n-th group's maximum); what
+// passes it goes to a buffer in LDS, a key's rank being the number of larger ones there.
+// Only rows of very many equal values pass more than the buffer holds: they are taken one
+// by one.
 #include "common.h"
 #include "kernels.h"
 
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int CAND = 192;    // keys of a wavefront's buffer: room for 64 more while it holds up to 128
+constexpr int CAND = 1024;   // keys of the buffer
 constexpr int STEP = 8;      // keys read at a time, the last ones padded with 0
 constexpr int GROUP = 16;    // vectors of a group
 constexpr int LDS_GROUPS = 4096;  // groups of a row whose maxima stay in LDS where one workgroup has the row
@@ -89,64 +91,6 @@ __device__ __forceinline__ Sums block_sums(Sums s, float* lds) {
   return r;
 }
 
-// The n best keys of a wavefront's stream; all lanes call together.
-struct Best {
-  u64* buf;  // LDS, CAND + STEP keys
-  int n, count;
-  u64 least;    // the n-th key: nothing below it matters (0: fewer than n so far)
-  float bound;  // logits below it cannot pass
-  __device__ __forceinline__ Best(u64* b, int n_) : buf(b), n(n_), count(0), least(0), bound(-INFINITY) {}
-  template <int SLOTS>
-  __device__ __forceinline__ void rank_and_place() {
-    const int lane = threadIdx.x & 63;
-    u64 k[SLOTS];
-    int rank[SLOTS];
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i) {
-      k[i] = lane + 64 * i < count ? buf[lane + 64 * i] : 0;
-      rank[i] = 0;
-    }
-    if (lane < STEP) buf[count + lane] = 0;
-    wave_sync();
-    for (int j = 0; j < count; j += STEP) {
-      u64 o[STEP];
-#pragma unroll
-      for (int u = 0; u < STEP; ++u) o[u] = buf[j + u];
-#pragma unroll
-      for (int u = 0; u < STEP; ++u)
-#pragma unroll
-        for (int i = 0; i < SLOTS; ++i) rank[i] += o[u] > k[i];
-    }
-    wave_sync();
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i)
-      if (lane + 64 * i < count && rank[i] < n) buf[rank[i]] = k[i];
-    wave_sync();
-  }
-  __device__ __forceinline__ void cut() {
-    if (count <= 64) rank_and_place<1>();
-    else rank_and_place<CAND / 64>();
-    count = count < n ? count : n;
-    if (count == n) {
-      least = buf[n - 1];
-      bound = value_of(least);
-    }
-  }
-  // the keys of the lanes that have one (0: none)
-  __device__ __forceinline__ void add(u64 k) {
-    if (count > CAND - 64) cut();
-    const bool in = k > least;
-    const u64 mask = __ballot(in);
-    if (in) buf[count + __builtin_amdgcn_mbcnt_hi(mask >> 32, __builtin_amdgcn_mbcnt_lo(mask, 0))] = k;
-    count += __popcll(mask);
-  }
-  // LDS accesses of one wavefront run in order; this keeps the compiler to it
-  static __device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-};
-
 // v[k] becomes the largest of its 16 lanes of a DPP row, in all of them
 template <int CTRL, int K>
 __device__ __forceinline__ void row_max_step(float (&v)[K]) {
@@ -162,64 +106,83 @@ __device__ __forceinline__ void row_max(float (&v)[K]) {
   row_max_step<0x121>(v);
 }
 
-// The n best of the wavefronts' lists, sorted, to top[0 .. n) (0: none left).
-__device__ __forceinline__ void block_top(Best& b, u64 (*bufs)[CAND + STEP], u64* top) {
-  b.cut();
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-  if (lane >= b.count && lane < b.n + STEP) bufs[wave][lane] = 0;
-  if (t < 32) top[t] = 0;
+struct Select {
+  u64 buf[CAND + STEP];
+  u64 top[32];      // the result, sorted; 0: none left
+  int group[32];    // the n best groups
+  u64 best[WAVES];
+  float bound[64];
+  int count;
+};
+
+// The n best of get(i), i < cnt (-inf: none), at keys of index(i), to sel.top, by the whole
+// workgroup. At least n of them, or all, reach `bound`.
+template <typename G, typename I>
+__device__ __forceinline__ void select_best(Select& sel, int n, int cnt, float bound, G get, I index) {
+  const int t = threadIdx.x;
+  if (t == 0) sel.count = 0;
+  __syncthreads();  // top may have been read until here
+  if (t < 32) sel.top[t] = 0;
+  constexpr int K = 8;  // reads in flight
+  for (int base = t; base < cnt; base += K * THREADS) {
+    float x[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = base + k * THREADS < cnt ? get(base + k * THREADS) : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (x[k] >= bound && x[k] > -INFINITY) {
+        const int at = atomicAdd(&sel.count, 1);
+        if (at < CAND) sel.buf[at] = key_of(x[k], index(base + k * THREADS));
+      }
+  }
   __syncthreads();
-  for (int i = t; i < WAVES * b.n; i += THREADS) {
-    const u64 k = bufs[i / b.n][i % b.n];
-    int rank = 0;
-    for (int w = 0; w < WAVES; ++w)
-      for (int j = 0; j < b.n; j += STEP) {
+  const int c = sel.count;
+  if (c <= CAND) {
+    if (t < STEP) sel.buf[c + t] = 0;
+    __syncthreads();
+    for (int i = t; i < c; i += THREADS) {
+      const u64 k = sel.buf[i];
+      int rank = 0;
+      for (int j = 0; j < c; j += STEP) {
         u64 o[STEP];
 #pragma unroll
-        for (int u = 0; u < STEP; ++u) o[u] = bufs[w][j + u];
+        for (int u = 0; u < STEP; ++u) o[u] = sel.buf[j + u];
 #pragma unroll
         for (int u = 0; u < STEP; ++u) rank += o[u] > k;
       }
-    if (k && rank < b.n) top[rank] = k;
+      if (rank < n) sel.top[rank] = k;
+    }
+  } else {
+    u64 last = ~0ull;
+    for (int r = 0; r < n && last; ++r) {
+      u64 best = 0;
+      for (int i = t; i < cnt; i += THREADS) {
+        const float x = get(i);
+        const u64 k = x > -INFINITY ? key_of(x, index(i)) : 0;
+        if (k < last && k > best) best = k;
+      }
+      for (int o = 32; o > 0; o >>= 1) {
+        const u64 k = __shfl_xor(best, o);
+        best = k > best ? k : best;
+      }
+      if ((t & 63) == 0) sel.best[t >> 6] = best;
+      __syncthreads();
+      last = sel.best[0];
+      for (int w = 1; w < WAVES; ++w) last = sel.best[w] > last ? sel.best[w] : last;
+      if (t == 0) sel.top[r] = last;
+      __syncthreads();
+    }
   }
   __syncthreads();
 }
 
-// The n best of x[k] at index i0 + k step (-inf: none), over the wavefront, into b. `lanes`: groups
-// of lanes for the first call's bound.
-template <int K>
-__device__ __forceinline__ void consider(Best& b, const float (&x)[K], int i0, int step, bool first, int lanes) {
-  float hi = x[0];
-#pragma unroll
-  for (int k = 1; k < K; ++k) hi = fmaxf(hi, x[k]);
-  if (first) {
-    float g = hi;
-    for (int o = 32; o >= lanes; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
-    int higher = 0;
-    if (lanes == 64) {
-#pragma unroll
-      for (int i = 0; i < 64; ++i) higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i)) > g;
-    } else {
-      for (int i = 0; i < lanes; ++i)
-        higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i)) > g;
-    }
-    b.bound = -wave_max(higher < b.n ? -g : -INFINITY);
-  }
-  if (!__any(hi >= b.bound && hi > -INFINITY)) return;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const bool in = x[k] >= b.bound && x[k] > -INFINITY;
-    if (__any(in)) b.add(in ? key_of(x[k], i0 + k * step) : 0);
-  }
-  if (first) b.cut();
-}
-
-// The row's results from its sums and its groups' maxima (LDS or workspace), by the whole workgroup.
+// The row's results from its sums and its groups' maxima (LDS or workspace), by the whole
+// workgroup. `lanes`: groups of lanes for the bound of the maxima.
 template <typename T>
 __device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, const float* maxima, int lanes,
-                                       u64 (*bufs)[CAND + STEP], u64* top) {
-  constexpr int VE = 16 / sizeof(T), GT = GROUP * VE, PER = GT / 64;  // tokens of a group, of a lane
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, n = a.n_top;
+                                       Select& sel) {
+  constexpr int VE = 16 / sizeof(T), GT = GROUP * VE;  // tokens of a group
+  const int t = threadIdx.x, n = a.n_top;
   const T* const x0 = (const T*)a.logits + row * a.ld;
   const bool bad = s.S != s.S, none = s.m == -INFINITY;
   const float l2 = log2f(s.S);
@@ -241,42 +204,42 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, co
   if (n == 0) return;
   const int off = (int)(((uintptr_t)x0 / sizeof(T)) % VE);
   const int groups = (off + a.vocab + GT - 1) / GT;
-  {
-    constexpr int K = 4;
-    Best b(bufs[wave], n);
-    for (int base = 0; base < groups; base += THREADS * K) {
-      float x[K];
+  float g = -INFINITY;
+  for (int i = t; i < groups; i += 4 * THREADS) {
+    float x[4];
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int i = base + k * THREADS + t;
-        x[k] = i < groups ? maxima[i] : -INFINITY;
-      }
-      consider(b, x, base + t, THREADS, base == 0, lanes);
-    }
-    block_top(b, bufs, top);
+    for (int k = 0; k < 4; ++k) x[k] = i + k * THREADS < groups ? maxima[i + k * THREADS] : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g = fmaxf(g, x[k]);
   }
-  // the groups' logits: wavefront w has the groups w, w + 4, ...
-  constexpr int MINE = 32 / WAVES;
-  Best b(bufs[wave], n);
-  if (top[n - 1]) b.bound = value_of(top[n - 1]);
-  float y[MINE][PER];
-  int tok[MINE];
+  // `lanes` groups over the workgroup, lanes / WAVES of each wavefront; every wavefront ranks them all
+  const int own = lanes / WAVES, lane = t & 63;
+  for (int o = 32; o >= own; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
+  if (lane < own) sel.bound[(t >> 6) * own + lane] = g;
+  __syncthreads();
+  g = lane < lanes ? sel.bound[lane] : -INFINITY;
+  int higher = 0;
+  for (int i = 0; i < lanes; i += 4)  // a multiple of 4
 #pragma unroll
-  for (int g = 0; g < MINE; ++g) {
-    const int at = wave + WAVES * g;
-    const u64 k = at < n ? top[at] : 0;
-    tok[g] = token_of(k) * GT + lane * PER - off;
-#pragma unroll
-    for (int e = 0; e < PER; ++e)
-      y[g][e] = k && (unsigned)(tok[g] + e) < (unsigned)a.vocab && tok[g] + e != a.exclude ? (float)x0[tok[g] + e]
-                                                                                           : -INFINITY;
-  }
-  __syncthreads();  // the lists are read, their buffers are free
-#pragma unroll
-  for (int g = 0; g < MINE; ++g) consider(b, y[g], tok[g], 1, false, lanes);
-  block_top(b, bufs, top);
+    for (int k = 0; k < 4; ++k)
+      higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i + k)) > g;
+  float bound = -wave_max(lane < lanes && higher < n ? -g : -INFINITY);
+  select_best(sel, n, groups, bound, [&](int i) { return maxima[i]; }, [&](int i) { return i; });
+  // the groups' logits
+  const int have = __popcll(__ballot(lane < n && sel.top[lane]));
+  bound = have == n ? value_of(sel.top[n - 1]) : -INFINITY;
+  if (t < n) sel.group[t] = token_of(sel.top[t]);
+  __syncthreads();
+  const auto token = [&](int i) { return sel.group[i / GT] * GT + i % GT - off; };
+  select_best(
+      sel, n, have * GT, bound,
+      [&](int i) {
+        const int k = token(i);
+        return (unsigned)k < (unsigned)a.vocab && k != a.exclude ? (float)x0[k] : -INFINITY;
+      },
+      token);
   if (t < n) {
-    const u64 k = top[t];
+    const u64 k = sel.top[t];
     const int64_t at = (int64_t)row * n + t;
     a.top_ids[at] = bad || k == 0 ? -1 : token_of(k);
     a.top_logprobs[at] = bad ? NAN : k == 0 ? -INFINITY : logprob(value_of(k));
@@ -294,8 +257,7 @@ logprobs_kernel(LogprobArgs a, int segs, int parts, int groups, int lanes) {
   constexpr int VE = 16 / sizeof(T), EPT = NV * VE, SEG = THREADS * EPT;
   typedef T vec __attribute__((ext_vector_type(VE)));
   __shared__ float sums[3 * WAVES];
-  __shared__ u64 bufs[WAVES][CAND + STEP];
-  __shared__ u64 top[32];
+  __shared__ Select sel;
   extern __shared__ float lds_maxima[];
   const int row = blockIdx.x / parts, part = blockIdx.x % parts, t = threadIdx.x;
   const int seg0 = (int)((int64_t)segs * part / parts), seg1 = (int)((int64_t)segs * (part + 1) / parts);
@@ -377,7 +339,7 @@ logprobs_kernel(LogprobArgs a, int segs, int parts, int groups, int lanes) {
   }
   s = block_sums(s, sums);
   if (parts == 1) {
-    finish<T>(a, row, s, maxima, lanes, bufs, top);
+    finish<T>(a, row, s, maxima, lanes, sel);
     return;
   }
   if (t == 0) ((Sums*)a.ws)[(int64_t)row * parts + part] = s;
@@ -387,13 +349,12 @@ logprobs_kernel(LogprobArgs a, int segs, int parts, int groups, int lanes) {
 template <typename T>
 __global__ void __launch_bounds__(THREADS) logprobs_join_kernel(LogprobArgs a, int parts, int groups, int lanes) {
   __shared__ float sums[3 * WAVES];
-  __shared__ u64 bufs[WAVES][CAND + STEP];
-  __shared__ u64 top[32];
+  __shared__ Select sel;
   const int row = blockIdx.x, t = threadIdx.x;
   Sums s{-INFINITY, 0.f, 0.f};
   if (t < parts) s = ((const Sums*)a.ws)[(int64_t)row * parts + t];
   s = block_sums(s, sums);
-  finish<T>(a, row, s, ws_maxima(a, parts, row, groups), lanes, bufs, top);
+  finish<T>(a, row, s, ws_maxima(a, parts, row, groups), lanes, sel);
 }
 
 int64_t groups_of(int64_t vocab, int elem) {
@@ -429,7 +390,7 @@ Cut cut_rows(int64_t rows, int64_t vocab, int elem) {
 
 template <typename T, int NV>
 hipError_t launch(const LogprobArgs& a, const Cut& c, hipStream_t s) {
-  int lanes = 1;  // at least twice n where there are as many
+  int lanes = WAVES;  // at least twice n where there are as many
   while (lanes < 64 && lanes < 2 * a.n_top) lanes *= 2;
   const int groups = (int)groups_of(a.vocab, sizeof(T));
   const int lds = a.n_top && c.parts == 1 && groups <= LDS_GROUPS ? groups * 4 : 0;

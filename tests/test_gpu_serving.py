@@ -405,6 +405,23 @@ def test_logprobs_ties(lp, dtype):
     check_score(lp, x, tokens, 0, 7)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [2, 1100])
+def test_logprobs_ties_long(lp, dtype, rows):
+    """More equal values than any buffer holds, in a long row and in rows that one workgroup has."""
+    V = 150000 if rows == 2 else 70000
+    x = torch.zeros((rows, V), dtype=dtype, device="cuda")
+    x[1] = -3.0
+    x[1, 5::1000] = 1.0
+    tokens = torch.zeros(rows, dtype=I32, device="cuda")
+    for n in (3, 32):
+        lo, en, ids, tl = score(lp, x, tokens, -1, n)
+        want = torch.arange(n, dtype=I32, device="cuda")
+        assert torch.equal(ids[0], want) and torch.equal(ids[1], 5 + 1000 * want)
+        assert (ids == want)[torch.arange(rows) != 1].all()
+        assert ((tl[0] + math.log(V)).abs() < 1e-4).all() and ((en[0] - math.log(V)).abs() < 1e-4).all()
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, F32])
 def test_logprobs_masked_rows(lp, dtype):
     """Masks of -inf and of the type's lowest value, rows with nothing left, with one token,
