@@ -106,6 +106,9 @@ __device__ __forceinline__ int key_limit(int p, const Div& block, int len) {
   return lim < len ? (int)lim : len;
 }
 
+// zero by its bits: this file is compiled without NaN in comparisons, and a NaN is not zero
+__device__ __forceinline__ bool is_zero(float v) { return (__float_as_uint(v) & 0x7fffffffu) == 0; }
+
 __device__ __forceinline__ float max_halves(float v) {
   const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
@@ -435,7 +438,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   if constexpr (WK == 1) {
     if (w0 + c < m1) {
       if (whole) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = is_zero(l) ? 0.f : 1.f / l;
         T* op = out + row * a.ld_out + head * D + 4 * h;
         typedef T vec4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -443,11 +446,11 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             vec4 w;
-            for (int e = 0; e < 4; ++e) w[e] = (T)(l == 0.f ? 0.f : o[db][4 * i + e] * inv);
+            for (int e = 0; e < 4; ++e) w[e] = (T)(is_zero(l) ? 0.f : o[db][4 * i + e] * inv);
             *(vec4*)(op + 32 * db + 8 * i) = w;
           }
         if (a.lse && h == 0)
-          a.lse[(int64_t)row * a.heads + head] = l == 0.f ? -INFINITY : (ref + log2f(l)) * ln2;
+          a.lse[(int64_t)row * a.heads + head] = is_zero(l) ? -INFINITY : (ref + log2f(l)) * ln2;
       } else {
         float* pp = part + (32 * wm + c) * D + 4 * h;
 #pragma unroll
@@ -496,7 +499,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
         const float rk = sr[(k * BM + rr) * 2];
         f[k] = rk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rk - top);
         // a part without keys has nothing to add (its l is 0, or NaN stays)
-        sum += f[k] == 0.f && rk == -INFINITY ? sr[(k * BM + rr) * 2 + 1] : f[k] * sr[(k * BM + rr) * 2 + 1];
+        sum += rk == -INFINITY ? sr[(k * BM + rr) * 2 + 1] : f[k] * sr[(k * BM + rr) * 2 + 1];
         for (int e = 0; e < E; e += 4) {
           const f32x4 v = *(const f32x4*)(so + (k * BM + rr) * LD + e0 + e);
           for (int u = 0; u < 4; ++u) acc[e + u] += rk == -INFINITY ? v[u] : f[k] * v[u];
@@ -504,16 +507,16 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
       }
       const int mm = m0 + rr, mq = quotient(mm, L.group);
       if (whole) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const float inv = is_zero(sum) ? 0.f : 1.f / sum;
         const int64_t r2 = q.start + mq;
         T* op = out + r2 * a.ld_out + (kvh * G + mm - mq * G) * D + e0;
         for (int e = 0; e < E; e += 8) {
           vec8 w;
-          for (int u = 0; u < 8; ++u) w[u] = (T)(sum == 0.f ? 0.f : acc[e + u] * inv);
+          for (int u = 0; u < 8; ++u) w[u] = (T)(is_zero(sum) ? 0.f : acc[e + u] * inv);
           *(vec8*)(op + e) = w;
         }
         if (a.lse && e0 == 0)
-          a.lse[r2 * a.heads + kvh * G + mm - mq * G] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * ln2;
+          a.lse[r2 * a.heads + kvh * G + mm - mq * G] = is_zero(sum) ? -INFINITY : (top + log2f(sum)) * ln2;
       } else {
         for (int e = 0; e < E; e += 4)
           *(f32x4*)(part + rr * D + e0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
@@ -578,7 +581,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
     for (int u = 0; u < UNROLL; ++u) {
       // a part without keys has nothing but zeros (or a NaN that stays)
       const float f = base + first + u * STEP >= parts ? 0.f : r[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r[u] - top);
-      if (f == 0.f) continue;
+      if (is_zero(f)) continue;
       sum += f * l[u];
       for (int e = 0; e < 4; ++e) acc[e] += f * v[u][e];
     }
@@ -597,15 +600,15 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
       for (int e = 0; e < 4; ++e) acc[e] += so[w][sub][e];
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = is_zero(sum) ? 0.f : 1.f / sum;
   if (lane < LP) {
     typedef T vec4 __attribute__((ext_vector_type(4)));
     vec4 w;
-    for (int e = 0; e < 4; ++e) w[e] = (T)(sum == 0.f ? 0.f : acc[e] * inv);
+    for (int e = 0; e < 4; ++e) w[e] = (T)(is_zero(sum) ? 0.f : acc[e] * inv);
     *(vec4*)((T*)a.out + row * a.ld_out + head * D + 4 * sub) = w;
   }
   if (a.lse && lane == 0)
-    a.lse[(int64_t)row * a.heads + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+    a.lse[(int64_t)row * a.heads + head] = is_zero(sum) ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -656,6 +659,7 @@ hipError_t launch(const PagedAttnArgs& a, const AttnLaunch& L, hipStream_t s) {
   constexpr int bytes = ring > join ? ring : join;
   static_assert(bytes <= 160 * 1024, "LDS of one CU");
   const int64_t n = (int64_t)L.slots * L.splits * a.pages.kv_heads;
+  if (n >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
   attn_kernel<T, D, WM, CAP><<<dim3((unsigned)n), dim3(256), bytes, s>>>(a, L);
   return hipGetLastError();
 }

@@ -229,6 +229,69 @@ def test_attention_seen_values(lp, n, m):
     assert torch.isfinite(out[:, :, rest]).all()
 
 
+@pytest.mark.parametrize("n,m", [(1, 300), (150, 300), (1, 5000)])
+@pytest.mark.parametrize("what", ["k", "q"])
+def test_attention_nan_scores(lp, n, m, what):
+    """A NaN score reaches the rows that see it, and no other."""
+    b = ref.Batch([(n, m), (2, 40)], 32, 1, 128, BF, 23)
+    q = randn(5, (n + 2, 2, 128), BF)
+    at = n // 3 if n > 1 else 0  # row of sequence 0
+    if what == "k":
+        p = m - n + at
+        b.k[b.table[0, p // 32].long(), 0, p % 32, 7] = math.nan
+        bad = torch.arange(n, device="cuda") >= at
+    else:
+        q[at, :, 9] = math.nan
+        bad = torch.arange(n, device="cuda") == at
+    out, lse = attend(lp, b, q, 1)
+    assert torch.isnan(out[:n][bad]).all() and torch.isnan(lse[:n][bad]).all()
+    assert torch.isfinite(out[:n][~bad]).all() and torch.isfinite(lse[:n][~bad]).all()
+    assert torch.isfinite(out[n:]).all()
+
+
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 2, 64), (28, 4, 128)])
+@pytest.mark.parametrize("block", [0, 1, 4])
+def test_attention_more_rows_than_keys(lp, heads, kv_heads, d, block):
+    """Rows at positions before 0 see nothing unless the attention is full; no keys at all."""
+    b = ref.Batch([(5, 3), (40, 7), (3, 0), (2, 20)], 16, kv_heads, d, BF, 3, fill=math.nan)
+    q = randn(5, (b.rows, heads, d), BF)
+    out, lse = check_attend(lp, b, q, block)
+    assert (out[45:48] == 0).all() and (lse[45:48] == -math.inf).all()
+
+
+def test_rows_before_the_first_sequence(lp):
+    """q_start need not begin at 0: rows before it stay as they are."""
+    b = ref.Batch([(2, 30), (33, 50)], 16, 2, 64, BF, 3)
+    q = randn(5, (b.rows, 4, 64), BF)
+    want, wlse = attend(lp, b, q)
+    q5 = torch.cat([q[:5], q])
+    b.q_start += 5
+    out, lse = attend(lp, b, q5)
+    assert torch.equal(out[5:], want) and torch.equal(lse[5:], wlse) and (out[:5] == 7).all()
+    got = torch.full_like(q5, 7.0)
+    kv = randn(6, (b.rows + 5, 2, 64), BF)
+    lp.lopa_paged_append(b.k, b.v, b.table, b.q_start, b.kv_len, q5, kv, kv, None, None, 0.0, 0.0, got)
+    assert torch.equal(got[5:], q) and (got[:5] == 7).all()
+    assert torch.equal(b.v[b.table[0, 1].long(), :, 13], kv[6])  # row 6: position 29 of sequence 0
+
+
+def test_append_more_rows_than_tokens(lp):
+    """Rows at positions before 0 have no slot: their queries are rotated, nothing is written."""
+    b = ref.Batch([(4, 20)], 16, 2, 64, HF, 3)
+    b.kv_len[0] = 2
+    q, kv = randn(1, (4, 4, 64), HF), randn(2, (4, 2, 64), HF)
+    k0 = b.k.clone()
+    out = torch.empty_like(q)
+    lp.lopa_paged_append(b.k, b.v, b.table, b.q_start, b.kv_len, q, kv, kv, None, None, 0.0, 1e4, out)
+    b.lens = [(4, 2)]
+    wq, tq, wk, tk = ref.append(b, q, kv, kv, None, None, 0.0, 1e4)
+    ref.close(out, wq, tq)
+    page = b.table[0, 0].long()
+    ref.close(b.k[page, :, :2].transpose(0, 1), wk[2:], tk[2:])
+    b.k[page, :, :2] = k0[page, :, :2]
+    assert torch.equal(b.k, k0)
+
+
 def test_attention_strides_and_tail(lp):
     """q and out as views of wider rows; rows behind the last sequence stay as they were."""
     b = ref.Batch(LENS["mixed"], 32, 2, 64, BF, 3, fill=math.nan)
