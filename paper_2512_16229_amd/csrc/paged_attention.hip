@@ -44,7 +44,7 @@ template <>
 struct Num<__bf16> {
   typedef bf16x8 vec8;
   // numerators reach 2^(x - r) <= 2^LIM; a new reference is the maximum - SHIFT
-  static constexpr float SHIFT = 0.f, LIM = 8.f;
+  static constexpr float SHIFT = 0.f, LIM = 8.f, SCALE = 1.f;  // SCALE = 2^-SHIFT
   static constexpr uint16_t MAX = 0x7f7f;  // bits of the largest finite value
   static __device__ __forceinline__ f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -53,7 +53,7 @@ struct Num<__bf16> {
 template <>
 struct Num<_Float16> {
   typedef f16x8 vec8;
-  static constexpr float SHIFT = 8.f, LIM = 14.f;
+  static constexpr float SHIFT = 8.f, LIM = 14.f, SCALE = 0.00390625f;
   static constexpr uint16_t MAX = 0x7bff;
   static __device__ __forceinline__ f32x16 mfma(vec8 a, vec8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
@@ -108,6 +108,12 @@ __device__ __forceinline__ int key_limit(int p, const Div& block, int len) {
 
 // zero by its bits: this file is compiled without NaN in comparisons, and a NaN is not zero
 __device__ __forceinline__ bool is_zero(float v) { return (__float_as_uint(v) & 0x7fffffffu) == 0; }
+
+// ln of a row's sum of 2^x: the reference's shift is taken from both parts exactly
+template <typename N>
+__device__ __forceinline__ float log_sum(float ref, float l) {
+  return is_zero(l) ? -INFINITY : ((ref + N::SHIFT) + log2f(l * N::SCALE)) * 0.69314718f;
+}
 
 __device__ __forceinline__ float max_halves(float v) {
   const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -350,13 +356,38 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
     ids2 = page_of(it + 3);
     const int kt = (first + it * WK) * KT;
     if constexpr (CAP) {
-      // log2(e) cap tanh(s / cap), tanh(y) = 1 - 2 / (e^(2y) + 1)
-      const float in = 2.f * sc / a.softcap, out = LOG2E * a.softcap;
+      // log2(e) cap tanh(y), y = s / cap: for |y| <= TINY by its series (the next term is below
+      // 2^-26), else as 1 - 2 / (e^(2y) + 1), which is off by 2^-24 of the cap itself
+      constexpr float TINY = 0.35f;
+      const float in = (a.scale == 0.f ? 1.f : fabsf(a.scale)) / a.softcap, out = LOG2E * a.softcap;
+      float big = 0.f;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          x[nb][i] = out - 2.f * out * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x[nb][i] * in) + 1.f);
+        for (int i = 0; i < 16; ++i) x[nb][i] *= in, big = fmaxf(big, fabsf(x[nb][i]));
+      const auto series = [](float y) {
+        const float z = y * y;
+        float t = fmaf(z, -1382.f / 155925.f, 62.f / 2835.f);
+        t = fmaf(z, t, -17.f / 315.f);
+        t = fmaf(z, t, 2.f / 15.f);
+        t = fmaf(z, t, -1.f / 3.f);
+        return fmaf(y * z, t, y);
+      };
+      if (!__any(big > TINY)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[nb][i] = series(x[nb][i]) * out;
+      } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float y = x[nb][i], s = series(y);
+            const float w = 1.f - 2.f * __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.f * LOG2E)) + 1.f);
+            x[nb][i] = (fabsf(y) > TINY ? w : s) * out;
+          }
+      }
     }
     const float mul = CAP ? 1.f : sc;
     if (have != ALL || kt + KT > lim_min) {
@@ -433,7 +464,6 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   if (!whole)
     part = L.ws + (((int64_t)slot * Hkv + kvh) * L.splits + split) * part_floats<D>(BM);
   T* const out = (T*)a.out;
-  const float ln2 = 0.69314718f;
 
   if constexpr (WK == 1) {
     if (w0 + c < m1) {
@@ -450,7 +480,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
             *(vec4*)(op + 32 * db + 8 * i) = w;
           }
         if (a.lse && h == 0)
-          a.lse[(int64_t)row * a.heads + head] = is_zero(l) ? -INFINITY : (ref + log2f(l)) * ln2;
+          a.lse[(int64_t)row * a.heads + head] = log_sum<N>(ref, l);
       } else {
         float* pp = part + (32 * wm + c) * D + 4 * h;
 #pragma unroll
@@ -516,7 +546,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
           *(vec8*)(op + e) = w;
         }
         if (a.lse && e0 == 0)
-          a.lse[r2 * a.heads + kvh * G + mm - mq * G] = is_zero(sum) ? -INFINITY : (top + log2f(sum)) * ln2;
+          a.lse[r2 * a.heads + kvh * G + mm - mq * G] = log_sum<N>(top, sum);
       } else {
         for (int e = 0; e < E; e += 4)
           *(f32x4*)(part + rr * D + e0 + e) = f32x4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
@@ -608,7 +638,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
     *(vec4*)((T*)a.out + row * a.ld_out + head * D + 4 * sub) = w;
   }
   if (a.lse && lane == 0)
-    a.lse[(int64_t)row * a.heads + head] = is_zero(sum) ? -INFINITY : (top + log2f(sum)) * 0.69314718f;
+    a.lse[(int64_t)row * a.heads + head] = log_sum<Num<T>>(top, sum);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -84,6 +84,24 @@ def test_attention_softcap(lp, lens, dtype, softcap):
     check_attend(lp, b, q, 1, softcap)
 
 
+@pytest.mark.parametrize("std", [0.01, 0.3, 3.0, 30.0])
+def test_attention_softcap_relative(lp, std):
+    """Scores far below the cap keep their relative accuracy: one key, whose lse is the capped score
+    (a sum of d products, a factor, the series or the quotient: within (d + 24) U32 of sum |q k|)."""
+    b = ref.Batch([(1, 1)] * 40, 16, 1, 64, HF, 5)
+    q = randn(4, (40, 2, 64), HF, std)
+    _, lse = attend(lp, b, q, 1, 50.0)
+    k = b.k[b.table[:, 0].long(), 0, 0].double()
+    s = (q.double() * k[:, None]).sum(-1) / 8
+    mag = (q.double() * k[:, None]).abs().sum(-1) / 8
+    want = 50 * torch.tanh(s / 50)
+    # past TINY of the cap the quotient's error counts against the cap. An fp16 numerator is
+    # 2^(8 + d), d the rounding of the reference (score - 8: at most half a step of 8 to 16, 2^-21):
+    # an exponential and a logarithm of 2^-23 relative each, on values within 2^-21 of 2^8 and 1,
+    # bring 2^-22 / ln 2 into log2 l, and so 2^-22 into lse
+    ref.close(lse, want, (64 + 24) * ref.U32 * mag + torch.where(s.abs() > 15, 8 * ref.U32 * 50, 0.0) + 2 ** -22)
+
+
 @pytest.mark.parametrize("m", [1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 257, 1023, 4097])
 @pytest.mark.parametrize("n", [1, 5, 40])
 def test_attention_lengths(lp, m, n):
