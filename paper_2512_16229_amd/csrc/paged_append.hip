@@ -13,7 +13,8 @@
 // needs no exchange and the norm one sum over the d / 16 lanes of a head. The
 // angles depend on the row and the pair only, and cost more than a head: a
 // wavefront computes them once for `per_wave` groups of heads of its row, the next
-// group's loads in flight.
+// group's loads in flight (8192 rows of 28 + 2 x 4 heads of 128, 151 MB: 36 us, 4.2 TB/s;
+// with one group a wavefront 55; one row 4.4 us).
 #include "paged.h"
 
 #include <algorithm>

@@ -556,6 +556,22 @@ def test_logprobs_strides(lp, dtype, offset, pad):
     check_score(lp, x, tokens, 9, 20)
 
 
+def test_logprobs_many_long_rows(lp):
+    """Rows that one workgroup has each, with more groups of tokens than its LDS keeps maxima of."""
+    R, V = 1100, 600001
+    x = torch.empty((R, V), dtype=BF, device="cuda")
+    for r in range(0, R, 100):
+        x[r:r + 100] = randn(r, (100, V), BF, 3.0)
+    tokens = torch.randint(0, V, (R,), generator=gen(1), device="cuda").to(I32)
+    lo, en, ids, tl = score(lp, x, tokens, 7, 12)
+    some = torch.tensor([0, 1, 513, 1098, 1099], device="cuda")
+    wl, we, wi, wt, rel = ref.logprobs(x[some], tokens[some], 7, 12)
+    ref.close(lo[some], wl, rel + 8 * ref.U32 * wl.abs())
+    ref.close(en[some], we, 2 * rel * (1 + we.abs()))
+    assert torch.equal(ids[some], wi)
+    ref.close(tl[some], wt, rel[:, None] + 8 * ref.U32 * wt.abs())
+
+
 def test_logprobs_far_rows(lp):
     """A row more than 2^32 elements behind the first."""
     V, ld = 4000, 2 ** 31 + 16
