@@ -6,17 +6,26 @@
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-// the sequence of a row: the last one that starts at or before it. All lanes of a
-// wavefront call it with the same row; starts are read 64 at a time. -1: none.
-__device__ __forceinline__ int seq_of_row(const int32_t* q_start, int n_seq, int row) {
+// the last i in [0, n) with at(i), for a condition that holds for the first ones only; -1: none.
+// All lanes of a wavefront call together: 64 places are looked at at a time.
+template <typename F>
+__device__ __forceinline__ int last_that(int n, F at) {
   const int lane = threadIdx.x & 63;
-  int n = 0;
-  for (int base = 0; base < n_seq; base += 64) {
-    const int i = base + lane;
-    const bool at = i < n_seq && q_start[i] <= row;
-    n += __popcll(__ballot(at));
-  }
-  return __builtin_amdgcn_readfirstlane(n) - 1;
+  int lo = 0, stride;
+  do {
+    stride = (n + 63) >> 6;
+    const int i = lane * stride;
+    const int k = __builtin_amdgcn_readfirstlane(__popcll(__ballot(i < n && at(lo + i)))) - 1;
+    if (k < 0) return lo - 1;
+    lo += k * stride;
+    n = n - k * stride < stride ? n - k * stride : stride;
+  } while (stride > 1);
+  return lo;
+}
+
+// the sequence of a row: the last one that starts at or before it
+__device__ __forceinline__ int seq_of_row(const int32_t* q_start, int n_seq, int row) {
+  return last_that(n_seq, [&](int i) { return q_start[i] <= row; });
 }
 
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }

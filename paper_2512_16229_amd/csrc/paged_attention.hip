@@ -179,15 +179,8 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
 
   // which sequence and row tile
   int s = slot, tile = 0;
-  if (!L.single) {
-    int n = 0;
-    for (int base = 0; base < a.batch.n_seq; base += 64) {
-      const int i = base + lane;
-      const bool at = i < a.batch.n_seq && (int64_t)a.batch.q_start[i] * G / BM + i <= slot;
-      n += __popcll(__ballot(at));
-    }
-    s = __builtin_amdgcn_readfirstlane(n) - 1;
-  }
+  if (!L.single)
+    s = last_that(a.batch.n_seq, [&](int i) { return (int64_t)a.batch.q_start[i] * G / BM + i <= slot; });
   Seq q;
   if (!read_seq(a, s, q)) return;
   if (!L.single) tile = slot - (int)((int64_t)q.start * G / BM + s);

@@ -277,6 +277,25 @@ def test_attention_more_rows_than_keys(lp, heads, kv_heads, d, block):
     assert (out[45:48] == 0).all() and (lse[45:48] == -math.inf).all()
 
 
+@pytest.mark.parametrize("n_seq", [63, 64, 65, 130, 2000])
+def test_many_sequences(lp, n_seq):
+    """Batches of many short sequences, some without rows, one long: attention and append find
+    each row's own."""
+    lens = [((i * 7) % 4, 3 + i % 50) for i in range(n_seq)]
+    lens[n_seq // 3] = (150, 160)
+    b = ref.Batch(lens, 16, 1, 64, BF, 3)
+    q = randn(5, (b.rows, 2, 64), BF)
+    check_attend(lp, b, q, 1)
+    kv = randn(6, (b.rows, 1, 64), BF)
+    out = torch.empty_like(q)
+    lp.lopa_paged_append(b.k, b.v, b.table, b.q_start, b.kv_len, q, kv, kv, None, None, 0.0, 0.0, out)
+    assert torch.equal(out, q)
+    seq = torch.tensor([s for s, (n, m) in enumerate(lens) for _ in range(n)], device="cuda")
+    pos = torch.tensor([p for n, m in lens for p in range(m - n, m)], device="cuda")
+    page = b.table[seq, pos // 16].long()
+    assert torch.equal(b.k[page, :, pos % 16], kv) and torch.equal(b.v[page, :, pos % 16], kv)
+
+
 def test_rows_before_the_first_sequence(lp):
     """q_start need not begin at 0: rows before it stay as they are."""
     b = ref.Batch([(2, 30), (33, 50)], 16, 2, 64, BF, 3)
