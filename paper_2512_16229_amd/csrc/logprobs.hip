@@ -33,7 +33,7 @@
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int CAND = 1024;   // keys of the buffer
+constexpr int CAND = 512;    // keys of the buffer (ranking more takes longer than taking n one by one)
 constexpr int STEP = 8;      // keys read at a time, the last ones padded with 0
 constexpr int GROUP = 16;    // vectors of a group
 constexpr int LDS_GROUPS = 4096;  // groups of a row whose maxima stay in LDS where one workgroup has the row
@@ -116,6 +116,31 @@ struct Select {
   float bound[64];
   int count;
 };
+
+// A bound that at least n of get(i), i < cnt, reach (or -inf): the n-th largest maximum of `lanes`
+// groups of lanes over the workgroup, lanes / WAVES of each wavefront; every wavefront ranks them all.
+template <typename G>
+__device__ __forceinline__ float nth_bound(Select& sel, int n, int lanes, int cnt, G get) {
+  const int t = threadIdx.x, lane = t & 63, own = lanes / WAVES;
+  float g = -INFINITY;
+  for (int i = t; i < cnt; i += 4 * THREADS) {
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = i + k * THREADS < cnt ? get(i + k * THREADS) : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g = fmaxf(g, x[k]);
+  }
+  for (int o = 32; o >= own; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
+  if (lane < own) sel.bound[(t >> 6) * own + lane] = g;
+  __syncthreads();
+  g = lane < lanes ? sel.bound[lane] : -INFINITY;
+  int higher = 0;
+  for (int i = 0; i < lanes; i += 4)  // a multiple of 4
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i + k)) > g;
+  return -wave_max(lane < lanes && higher < n ? -g : -INFINITY);
+}
 
 // The n best of get(i), i < cnt (-inf: none), at keys of index(i), to sel.top, by the whole
 // workgroup. At least n of them, or all, reach `bound`.
@@ -206,40 +231,23 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int row, Sums s, co
   if (n == 0) return;
   const int off = (int)(((uintptr_t)x0 / sizeof(T)) % VE);
   const int groups = (off + a.vocab + GT - 1) / GT;
-  float g = -INFINITY;
-  for (int i = t; i < groups; i += 4 * THREADS) {
-    float x[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = i + k * THREADS < groups ? maxima[i + k * THREADS] : -INFINITY;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) g = fmaxf(g, x[k]);
-  }
-  // `lanes` groups over the workgroup, lanes / WAVES of each wavefront; every wavefront ranks them all
-  const int own = lanes / WAVES, lane = t & 63;
-  for (int o = 32; o >= own; o >>= 1) g = fmaxf(g, __shfl_xor(g, o));
-  if (lane < own) sel.bound[(t >> 6) * own + lane] = g;
-  __syncthreads();
-  g = lane < lanes ? sel.bound[lane] : -INFINITY;
-  int higher = 0;
-  for (int i = 0; i < lanes; i += 4)  // a multiple of 4
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      higher += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i + k)) > g;
-  float bound = -wave_max(lane < lanes && higher < n ? -g : -INFINITY);
-  select_best(sel, n, groups, bound, [&](int i) { return maxima[i]; }, [&](int i) { return i; });
+  const int lane = t & 63;
+  const auto maximum = [&](int i) { return maxima[i]; };
+  float bound = nth_bound(sel, n, lanes, groups, maximum);
+  select_best(sel, n, groups, bound, maximum, [](int i) { return i; });
   // the groups' logits
   const int have = __popcll(__ballot(lane < n && sel.top[lane]));
-  bound = have == n ? value_of(sel.top[n - 1]) : -INFINITY;
+  const float last = have == n ? value_of(sel.top[n - 1]) : 0.f;
   if (t < n) sel.group[t] = token_of(sel.top[t]);
   __syncthreads();
   const auto token = [&](int i) { return sel.group[i / GT] * GT + i % GT - off; };
-  select_best(
-      sel, n, have * GT, bound,
-      [&](int i) {
-        const int k = token(i);
-        return (unsigned)k < (unsigned)a.vocab && k != a.exclude ? (float)x0[k] : -INFINITY;
-      },
-      token);
+  const auto logit = [&](int i) {
+    const int k = token(i);
+    return (unsigned)k < (unsigned)a.vocab && k != a.exclude ? (float)x0[k] : -INFINITY;
+  };
+  // fewer groups than n (a small vocabulary): a bound of their logits
+  bound = have == n ? last : nth_bound(sel, n, lanes, have * GT, logit);
+  select_best(sel, n, have * GT, bound, logit, token);
   if (t < n) {
     const u64 k = sel.top[t];
     const int64_t at = (int64_t)row * n + t;
