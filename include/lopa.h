@@ -421,9 +421,9 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
  *   NULL)
  * A row that sees no key gives zeros and lse = -inf. Keys that a row does not see
  * have no part in it, whatever they hold (NaN and infinities too). q and out
- * [rows][heads][head_dim] of the pages' type as in lopa_paged_append. Products of
- * that type are summed in fp32; the softmax is fp32, its numerators are rounded to
- * the type for the product with V.
+ * [rows][heads][head_dim] of the pages' type as in lopa_paged_append, with no
+ * memory in common. Products of that type are summed in fp32; the softmax is fp32,
+ * its numerators are rounded to the type for the product with V.
  * max_rows and max_len bound the rows and the kv_len of a sequence; the launch is
  * laid out for them, so a captured call serves every batch within them. A sequence
  * past either bound is left out (its rows stay as they are).

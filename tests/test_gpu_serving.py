@@ -522,6 +522,22 @@ def test_logprobs_ties_long(lp, dtype, rows):
         assert ((tl[0] + math.log(V)).abs() < 1e-4).all() and ((en[0] - math.log(V)).abs() < 1e-4).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows,vocab,n", [(1, 31, 32), (6, 300, 13), (2, 696, 13), (9, 1024, 20), (1100, 1024, 32)])
+def test_logprobs_small_vocabularies(lp, dtype, rows, vocab, n):
+    """More top tokens than the vocabulary has groups of logits: random rows, equal ones, one
+    whose best lie side by side, one with fewer tokens left than asked for."""
+    x = randn(rows + vocab, (max(rows, 5), vocab), dtype, 3.0)
+    x[1] = 1.0
+    x[2] = torch.arange(vocab, device="cuda").to(dtype)
+    x[3] = -float("inf")
+    x[3, 2:: max(vocab // 5, 1)] = 2.0
+    x[4, vocab // 2 : vocab // 2 + 14] += 50.0
+    tokens = torch.arange(x.shape[0], device="cuda").remainder(vocab).to(I32)
+    check_score(lp, x, tokens, -1, n)
+    check_score(lp, x, tokens, vocab // 2, n)
+
+
 @pytest.mark.parametrize("dtype", [BF, HF, F32])
 def test_logprobs_masked_rows(lp, dtype):
     """Masks of -inf and of the type's lowest value, rows with nothing left, with one token,
