@@ -610,9 +610,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
     if (base == 0) top = wave_max(top);
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      // a part without keys has nothing but zeros (or a NaN that stays)
-      const float f = base + first + u * STEP >= parts ? 0.f : r[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r[u] - top);
-      if (is_zero(f)) continue;
+      if (base + first + u * STEP >= parts) continue;
+      // a part without keys has nothing but zeros (or a NaN that stays); a factor of zero keeps the
+      // NaN of a part far below the others (0 x NaN, 0 x infinity)
+      const float f = r[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r[u] - top);
       sum += f * l[u];
       for (int e = 0; e < 4; ++e) acc[e] += f * v[u][e];
     }

@@ -1,0 +1,47 @@
+"""The serving operators at the edges of what their header promises."""
+import math
+
+import pytest
+import torch
+
+import serving_ref as ref
+from test_gpu_serving import BF, attend, randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lp():
+    import paper_2512_16229_amd as lp
+    return lp
+
+
+# ------------------------------------------------------------------- attention
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("lens,heads,kv_heads,d", [([(1, 5000)], 4, 1, 128), ([(1, 70000)], 2, 2, 64),
+                                                   ([(700, 9000)], 2, 1, 128)])
+def test_values_seen_far_below_the_maximum(lp, what, lens, heads, kv_heads, d):
+    """A key that a row sees has its part however far its score lies below the largest: key 0 scores
+    about 220, the others 0. A NaN in a later key makes the row NaN, an infinite value of V is not
+    lost (its weight e^-220 is no zero; as an fp32 factor it is, and the product NaN)."""
+    (n, m), = lens
+    b = ref.Batch(lens, 64, kv_heads, d, BF, 5)
+    b.k.zero_()
+    q = randn(3, (1, 1, d), BF).expand(n, heads, d).contiguous()
+    page = b.table[0, 0].long()
+    b.k[page, :, 0] = q[0, 0] * (220 * d ** 0.5 / q[0, 0].float().square().sum()).to(BF)
+    out, lse = attend(lp, b, q, 1)
+    v0 = b.v[page, :, 0].repeat_interleave(heads // kv_heads, 0)  # the other weights are below 9000 e^-200
+    ref.close(out, v0.double().expand_as(out), 2.0 ** -7 * v0.abs().double())
+    assert torch.isfinite(lse).all() and (lse > 200).all()
+    p = m - n - 1 if n > 1 else m - 1  # seen by every row
+    at = b.table[0, p // 64].long()
+    pool = b.k if what == "k" else b.v
+    pool[at, :, p % 64, 3] = math.nan if what == "k" else math.inf
+    out, lse = attend(lp, b, q, 1)
+    if what == "k":
+        assert torch.isnan(out).all() and torch.isnan(lse).all()
+    else:
+        assert not torch.isfinite(out[..., 3]).any()
+        rest = [i for i in range(d) if i != 3]
+        assert torch.isfinite(out[..., rest]).all() and torch.isfinite(lse).all()
