@@ -409,6 +409,8 @@ def lopa_token_logprobs(logits, tokens, exclude, logprob=None, entropy=None, top
     """logits [rows][vocab] of bfloat16, float16 or float32 (free row stride); tokens [rows] with
     logprob [rows]; entropy [rows]; top_ids and top_logprobs [rows][n]; each output may be None.
     exclude: a token outside the support, or -1."""
+    if getattr(top_ids, "shape", None) != getattr(top_logprobs, "shape", None):
+        raise ValueError("top_ids and top_logprobs go together, of one shape: both or neither")
     dev = _on(logits, "logits")
     dtype = _DTYPES.get(logits.dtype)
     if dtype is None or logits.dim() != 2:
