@@ -17,9 +17,9 @@ ARCH = os.environ.get("LOPA_ARCH", "gfx950")
 SOURCES = ["api.cpp", "step_kernels.hip", "row_kernels.hip", "gemm.hip", "attention.hip",
            "noalloc.hip", "serving_api.cpp", "paged_append.hip", "paged_attention.hip", "logprobs.hip"]
 # attention: scores are never NaN, and without NaN semantics the maximum of
-# scores needs no quieting of its operands
-# (paged: a NaN only passes through products, sums and exponentials there)
-EXTRA_FLAGS = {"attention.hip": ["-fno-honor-nans"], "paged_attention.hip": ["-fno-honor-nans"]}
+# scores needs no quieting of its operands (paged_attention.hip hands NaN on to
+# the rows that see it, and is compiled with NaN semantics)
+EXTRA_FLAGS = {"attention.hip": ["-fno-honor-nans"]}
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          # no packed-fp32 instructions in device code
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -114,13 +114,10 @@ __device__ __forceinline__ int key_limit(int p, const Div& block, int len) {
   return lim < len ? (int)lim : len;
 }
 
-// zero by its bits: this file is compiled without NaN in comparisons, and a NaN is not zero
-__device__ __forceinline__ bool is_zero(float v) { return (__float_as_uint(v) & 0x7fffffffu) == 0; }
-
 // ln of a row's sum of 2^x: the reference's shift is taken from both parts exactly
 template <typename N>
 __device__ __forceinline__ float log_sum(float ref, float l) {
-  return is_zero(l) ? -INFINITY : ((ref + N::SHIFT) + log2f(l * N::SCALE)) * 0.69314718f;
+  return l == 0.f ? -INFINITY : ((ref + N::SHIFT) + log2f(l * N::SCALE)) * 0.69314718f;
 }
 
 __device__ __forceinline__ float max_halves(float v) {
@@ -469,7 +466,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   if constexpr (WK == 1) {
     if (w0 + c < m1) {
       if (whole) {
-        const float inv = is_zero(l) ? 0.f : 1.f / l;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         T* op = out + row * a.ld_out + head * D + 4 * h;
         typedef T vec4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -477,7 +474,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             vec4 w;
-            for (int e = 0; e < 4; ++e) w[e] = (T)(is_zero(l) ? 0.f : o[db][4 * i + e] * inv);
+            for (int e = 0; e < 4; ++e) w[e] = (T)(l == 0.f ? 0.f : o[db][4 * i + e] * inv);
             *(vec4*)(op + 32 * db + 8 * i) = w;
           }
         if (a.lse && h == 0)
@@ -538,12 +535,12 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
       }
       const int mm = m0 + rr, mq = quotient(mm, L.group);
       if (whole) {
-        const float inv = is_zero(sum) ? 0.f : 1.f / sum;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int64_t r2 = q.start + mq;
         T* op = out + r2 * a.ld_out + (kvh * G + mm - mq * G) * D + e0;
         for (int e = 0; e < E; e += 8) {
           vec8 w;
-          for (int u = 0; u < 8; ++u) w[u] = (T)(is_zero(sum) ? 0.f : acc[e + u] * inv);
+          for (int u = 0; u < 8; ++u) w[u] = (T)(sum == 0.f ? 0.f : acc[e + u] * inv);
           *(vec8*)(op + e) = w;
         }
         if (a.lse && e0 == 0)
@@ -632,11 +629,11 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
       for (int e = 0; e < 4; ++e) acc[e] += so[w][sub][e];
     }
   }
-  const float inv = is_zero(sum) ? 0.f : 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
   if (lane < LP) {
     typedef T vec4 __attribute__((ext_vector_type(4)));
     vec4 w;
-    for (int e = 0; e < 4; ++e) w[e] = (T)(is_zero(sum) ? 0.f : acc[e] * inv);
+    for (int e = 0; e < 4; ++e) w[e] = (T)(sum == 0.f ? 0.f : acc[e] * inv);
     *(vec4*)((T*)a.out + row * a.ld_out + head * D + 4 * sub) = w;
   }
   if (a.lse && lane == 0)
