@@ -430,7 +430,8 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
  * workspace (device, 16-byte aligned): at least the bytes that
  * lopa_paged_attention_workspace gives for the same sizes, NULL if that is 0.
  * Errors: LOPA_ECAPACITY for max_len > table_ld * page_size, LOPA_ESHAPE for a
- * layout the kernels do not take or too small a workspace. */
+ * layout the kernels do not take, too small a workspace, or more work than a launch
+ * holds (never where rows * heads / 128 + n_seq * kv_heads < 2^24). */
 int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch, int32_t heads,
                          int32_t max_rows, int32_t max_len, const void* q, int64_t ld_q,
                          int32_t block, float scale, float softcap, void* out, int64_t ld_out,
@@ -455,7 +456,7 @@ int64_t lopa_paged_attention_workspace(int32_t heads, int32_t kv_heads, int32_t 
  * NaN or +inf has no distribution: logprob (of t >= 0), entropy and top_logprobs
  * are NaN and its ids -1.
  * logprob (with tokens), entropy and the top list (both arrays) may be NULL each.
- * 1 <= vocab <= 2^24, 0 <= n_top <= LOPA_MAX_TOP. fp32 throughout. */
+ * 0 <= rows < 2^24, 1 <= vocab <= 2^24, 0 <= n_top <= LOPA_MAX_TOP. fp32 throughout. */
 #define LOPA_MAX_TOP 32
 int lopa_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int32_t rows,
                         int32_t vocab, int32_t exclude, const int32_t* tokens, int32_t n_top,

@@ -196,6 +196,9 @@ struct AttnArgs {
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------- serving: paged cache
+// workgroups of 256 threads that a launch can have: its grid is counted in 32-bit work-items
+constexpr int64_t MAX_GROUPS = ((int64_t)1 << 24) - 1;
+
 struct AppendArgs {
   lopa_pages pages;
   lopa_paged_batch batch;
@@ -223,6 +226,7 @@ struct PagedPlan {
   } part[2];
   int n;
   int64_t bytes;  // workspace of all parts
+  bool fits;      // no launch has more than MAX_GROUPS workgroups
 };
 PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
                                int max_len);

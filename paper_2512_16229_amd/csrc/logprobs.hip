@@ -390,7 +390,7 @@ Cut cut_rows(int64_t rows, int64_t vocab, int elem) {
   c.nv = rows * segments(vocab, 4, elem) >= 256 ? 4 : 1;
   c.segs = (int)segments(vocab, c.nv, elem);
   int64_t least = INT64_MAX;
-  for (int p = 1; p <= c.segs && p <= PARTS; ++p) {
+  for (int p = 1; p <= c.segs && p <= PARTS && rows * p <= MAX_GROUPS; ++p) {
     const int64_t rounds = (rows * p + WGS - 1) / WGS, cost = rounds * ((c.segs + p - 1) / p) + (p > 1);
     if (cost < least) least = cost, c.parts = p;
     if (rounds > 1 && p >= 8) break;

@@ -652,8 +652,9 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 //   workgroups run in rounds of 256 occ;
 //   joining takes 4.5 and the parts' way to memory and back at 4 TB/s (8 branches of 32 rows over
 //   544 keys, wm = 4: 21 unsplit, 15 and 7.5 for joining in 5 parts).
+// No more than `groups` workgroups with split keys.
 PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, bool single, int64_t slots, int64_t tiles, int64_t seqs,
-                     int kv_heads, int d, int max_len) {
+                     int kv_heads, int d, int max_len, int64_t groups) {
   const int bm = 32 * wm, step = wm == 4 ? 64 : 128;
   const int occ = (wm == 4 ? 2 : 1) * (d == 64 ? 2 : 1);
   const double work = d == 64 ? 0.65 : 1.0;
@@ -662,6 +663,7 @@ PagedPlan::Part part(int wm, int64_t m_lo, int64_t m_hi, bool single, int64_t sl
   double least = 1e30;
   int64_t splits = 1;
   for (int64_t s = 1; s <= most && s <= 1024; s = s < 4 ? s + 1 : s * 4 / 3) {
+    if (s > 1 && slots * kv_heads * s > groups) break;
     const double iters = ceil_div(ceil_div(max_len, s), step), n = (double)items * s;
     const double load = n / (256 * occ), rounds = load <= 1.0 ? 1.0 : load + 0.5;
     const double streams = std::min(n, 256.0 * occ) * std::min(1.0, (double)seqs / tiles);
@@ -687,8 +689,7 @@ hipError_t launch(const PagedAttnArgs& a, const AttnLaunch& L, hipStream_t s) {
   constexpr int join = WK == 1 ? 0 : WK * BM * (D + 4 + 2) * 4;
   constexpr int bytes = ring > join ? ring : join;
   static_assert(bytes <= 160 * 1024, "LDS of one CU");
-  const int64_t n = (int64_t)L.slots * L.splits * a.pages.kv_heads;
-  if (n >= ((int64_t)1 << 31)) return hipErrorInvalidConfiguration;
+  const int64_t n = (int64_t)L.slots * L.splits * a.pages.kv_heads;  // <= MAX_GROUPS: plan.fits
   attn_kernel<T, D, WM, CAP><<<dim3((unsigned)n), dim3(256), bytes, s>>>(a, L);
   return hipGetLastError();
 }
@@ -739,11 +740,13 @@ hipError_t launch_all(const PagedAttnArgs& a, const PagedPlan& plan, hipStream_t
 PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
                                int max_len) {
   PagedPlan best{};
+  best.fits = true;
   if (n_seq < 1 || rows < 1 || max_rows < 1) return best;
   if (max_rows > rows) max_rows = rows;
   const int64_t G = heads / kv_heads, most = max_rows * G, all = INT64_MAX;
   const bool even = rows == (int64_t)n_seq * max_rows;
-  double least = 1e30;
+  const int64_t groups = rows <= MAX_GROUPS ? MAX_GROUPS : 0;  // joining takes one per row
+  double least = 1e300;
   for (int wm : {1, 2, 4}) {
     const int bm = 32 * wm;
     if (wm > 1 && most <= bm / 2) break;
@@ -753,14 +756,19 @@ PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int ro
     PagedPlan plan{};
     double us;
     if (wm == 1 || even) {
-      plan.part[plan.n++] = part(wm, 0, all, single, slots, tiles, n_seq, kv_heads, d, max_len);
+      plan.part[plan.n++] = part(wm, 0, all, single, slots, tiles, n_seq, kv_heads, d, max_len, groups);
       us = plan.part[0].us;
     } else {
       const int64_t large = std::max<int64_t>(1, std::min<int64_t>(n_seq, rows * G / most));
-      plan.part[plan.n++] = part(wm, 32, all, single, slots, ceil_div(rows * G, bm), large, kv_heads, d, max_len);
-      plan.part[plan.n++] = part(1, 0, 32, true, n_seq, n_seq, n_seq, kv_heads, d, max_len);
+      plan.part[plan.n++] =
+          part(wm, 32, all, single, slots, ceil_div(rows * G, bm), large, kv_heads, d, max_len, groups);
+      plan.part[plan.n++] = part(1, 0, 32, true, n_seq, n_seq, n_seq, kv_heads, d, max_len, groups);
       us = plan.part[0].us + plan.part[1].us + 6.0;
     }
+    plan.fits = true;
+    for (int i = 0; i < plan.n; ++i)
+      plan.fits &= plan.part[i].slots * plan.part[i].splits * kv_heads <= MAX_GROUPS;
+    if (!plan.fits) us += 1e200;  // only where no other does
     if (us < least) least = us, best = plan;
   }
   for (int i = 0; i < best.n; ++i) best.bytes += best.part[i].ws_bytes;

@@ -81,6 +81,12 @@ int check_bounds(int32_t heads, int32_t n_seq, int32_t rows, int32_t max_rows, i
   return LOPA_OK;
 }
 
+int check_fits(const PagedPlan& plan, int32_t heads, int32_t kv_heads, int32_t n_seq, int32_t rows) {
+  if (plan.fits) return LOPA_OK;
+  return lopa_fail(LOPA_ESHAPE, "%d rows of %d heads in %d sequences of %d K / V heads: more workgroups than a launch has",
+                   rows, heads, n_seq, kv_heads);
+}
+
 }  // namespace
 
 extern "C" {
@@ -124,7 +130,9 @@ int64_t lopa_paged_attention_workspace(int32_t heads, int32_t kv_heads, int32_t 
                                        int32_t max_len) {
   if (int e = check_heads(heads, kv_heads, head_dim)) return e;
   if (int e = check_bounds(heads, n_seq, rows, max_rows, max_len)) return e;
-  return paged_attention_plan(heads, kv_heads, head_dim, n_seq, rows, max_rows, max_len).bytes;
+  const PagedPlan plan = paged_attention_plan(heads, kv_heads, head_dim, n_seq, rows, max_rows, max_len);
+  if (int e = check_fits(plan, heads, kv_heads, n_seq, rows)) return e;
+  return plan.bytes;
 }
 
 int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch, int32_t heads,
@@ -146,6 +154,7 @@ int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch,
   if (int e = check_rows("out", out, ld_out, heads, d)) return e;
   const PagedPlan plan = paged_attention_plan(heads, pages->kv_heads, d, batch->n_seq, batch->rows,
                                               max_rows, max_len);
+  if (int e = check_fits(plan, heads, pages->kv_heads, batch->n_seq, batch->rows)) return e;
   if (plan.bytes > 0) {
     if (workspace_bytes < plan.bytes)
       return lopa_fail(LOPA_ESHAPE, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
@@ -168,9 +177,9 @@ int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch,
 }
 
 int64_t lopa_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top) {
-  if (rows < 0 || rows > MAX_BATCH_ROWS || vocab < 1 || vocab > MAX_VOCAB || n_top < 0 ||
+  if (rows < 0 || rows > MAX_GROUPS || vocab < 1 || vocab > MAX_VOCAB || n_top < 0 ||
       n_top > LOPA_MAX_TOP)
-    return lopa_fail(LOPA_ESHAPE, "rows %d, vocab %d or n_top %d outside [0, 2^24], [1, 2^24], [0, %d]",
+    return lopa_fail(LOPA_ESHAPE, "rows %d, vocab %d or n_top %d outside [0, 2^24 - 1], [1, 2^24], [0, %d]",
                      rows, vocab, n_top, LOPA_MAX_TOP);
   return logprobs_workspace(rows, vocab, n_top);
 }

@@ -38,3 +38,30 @@ def test_compiled_with_nan_semantics(src):
     flags = b.FLAGS + b.EXTRA_FLAGS.get(src, [])
     assert src in b.SOURCES
     assert not {"-ffast-math", "-ffinite-math-only", "-fno-honor-nans", "-Ofast"} & set(flags)
+
+
+# ------------------------------------------------ grids of 32-bit work-items
+def test_attention_of_more_work_than_a_launch_holds(lp):
+    """Sequences x K / V heads past 2^24 workgroups of 256 threads: refused before anything is
+    enqueued, by the workspace's size as by the call; just below it has a plan."""
+    f = lp.lib.lopa_paged_attention_workspace
+    assert f(512, 512, 64, 65535, 65535, 1, 100) == -2
+    p, b = api.pages(lp, kv_heads=512), api.batch(lp, n_seq=65535, rows=65535)
+    assert api.attend(lp, p, b, heads=512, ldq=512 * 64, ldo=512 * 64, max_rows=1) == -2, lp.lib.lopa_last_error()
+    assert f(256, 256, 64, 65535, 65535, 1, 100) == 0
+    assert f(1024, 1, 64, 65535, 1 << 20, 64, 100) >= 0
+
+
+def test_attention_splits_keys_within_a_launch(lp):
+    """Joining takes a workgroup per row: with 2^24 rows keys are not split."""
+    f = lp.lib.lopa_paged_attention_workspace
+    assert f(1, 1, 64, 2, (1 << 24) - 1, (1 << 24) - 2, 100000) > 0
+    assert f(1, 1, 64, 2, 1 << 24, (1 << 24) - 1, 100000) == 0
+
+
+def test_logprobs_rows(lp):
+    """Fewer than 2^24 rows; the parts of a row leave that many workgroups."""
+    f = lp.lib.lopa_token_logprobs_workspace
+    assert f(1 << 24, 100, 0) == -2 and api.logprobs(lp, rows=1 << 24) == -2
+    assert f((1 << 24) - 1, 100, 0) == 0
+    assert f((1 << 22) + 1, 30000, 0) < 12 * (1 << 24)  # 12 bytes a part
