@@ -195,12 +195,12 @@ int lopa_token_logprobs(const void* logits, int32_t dtype, int64_t ld, int32_t r
   if (ld < vocab) return lopa_fail(LOPA_EINVAL, "rows %lld elements apart, vocab %d", (long long)ld, vocab);
   if (exclude < -1 || exclude >= vocab)
     return lopa_fail(LOPA_EINVAL, "exclude %d outside [-1, %d)", exclude, vocab);
+  if (rows == 0) return LOPA_OK;  // arrays of no rows may be null
   if (!logprob != !tokens)
     return lopa_fail(LOPA_EINVAL, "tokens and logprob go together: both or neither");
   if (n_top ? !top_ids || !top_logprobs : top_ids || top_logprobs)
     return lopa_fail(LOPA_EINVAL, "n_top %d: %s top_ids and top_logprobs", n_top,
                      n_top ? "needs" : "takes no");
-  if (rows == 0) return LOPA_OK;
   if (!logits) return lopa_fail(LOPA_EINVAL, "null logits");
   if ((uintptr_t)logits % (dtype == LOPA_F32 ? 4 : 2))
     return lopa_fail(LOPA_EINVAL, "logits not aligned to their type");

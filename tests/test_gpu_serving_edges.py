@@ -45,3 +45,21 @@ def test_values_seen_far_below_the_maximum(lp, what, lens, heads, kv_heads, d):
         assert not torch.isfinite(out[..., 3]).any()
         rest = [i for i in range(d) if i != 3]
         assert torch.isfinite(out[..., rest]).all() and torch.isfinite(lse).all()
+
+
+def test_empty_batches(lp):
+    """No rows, with and without sequences: the calls return, and nothing changes."""
+    i32 = dict(dtype=torch.int32, device="cuda")
+    for n_seq in (0, 2):
+        b = ref.Batch([(1, 20), (1, 30)], 16, 2, 64, BF, 3)
+        k0, v0 = b.k.clone(), b.v.clone()
+        args = (b.table[:n_seq], torch.zeros(n_seq + 1, **i32), b.kv_len[:n_seq])
+        q, kv = (torch.empty((0, h, 64), dtype=BF, device="cuda") for h in (4, 2))
+        lp.lopa_paged_append(b.k, b.v, *args, q, kv, kv, None, None, 0.0, 1e4, torch.empty_like(q))
+        lp.lopa_paged_attention(q, b.k, b.v, *args, 0, 30, 1, 0.125, 0.0, torch.empty_like(q),
+                                torch.empty((0, 4), device="cuda"))
+        assert torch.equal(b.k, k0) and torch.equal(b.v, v0)
+    for n in (0, 3):
+        f = lambda *s: torch.empty(s, device="cuda")
+        lp.lopa_token_logprobs(f(0, 100), torch.empty(0, **i32), -1, f(0), f(0),
+                               torch.empty((0, n), **i32), f(0, n))

@@ -65,3 +65,14 @@ def test_logprobs_rows(lp):
     assert f(1 << 24, 100, 0) == -2 and api.logprobs(lp, rows=1 << 24) == -2
     assert f((1 << 24) - 1, 100, 0) == 0
     assert f((1 << 22) + 1, 30000, 0) < 12 * (1 << 24)  # 12 bytes a part
+
+
+# ----------------------------------------------------------------- empty batches
+def test_no_rows_need_no_arrays(lp):
+    """An empty batch is nothing to do, whichever arrays are null (empty tensors have no address)."""
+    none = dict(x=None, tokens=None, lo=None, en=None, ids=None, tl=None, ws=None, size=0)
+    assert api.logprobs(lp, rows=0, **none) == 0, lp.lib.lopa_last_error()
+    assert api.logprobs(lp, rows=0, ids=None, tl=None) == 0
+    empty = dict(q=None, out=None, b=api.batch(lp, rows=0))
+    assert api.attend(lp, **empty, ws=None, size=0) == 0 and api.append(lp, **empty, k=None, v=None) == 0
+    assert api.logprobs(lp, rows=0, n=33) == -2 and api.logprobs(lp, rows=0, exclude=100) == -1
