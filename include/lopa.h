@@ -402,8 +402,8 @@ typedef struct lopa_paged_batch {
  *   out_{j+h}   = y_{j+h} cos(a_j) + y_j sin(a_j)      a_j = p rope_theta^(-j/h)
  * (rope_theta = 0: no rotation), in fp32 with the angle reduced in fp64, rounded
  * once. Queries go to q_out [rows][heads][head_dim] (rows ld_out apart; q itself is
- * allowed), keys and the values as they are to their pages. Two rows that name the
- * same slot race. */
+ * allowed, other memory of q, k or v is not: LOPA_EINVAL), keys and the values as
+ * they are to their pages. Two rows that name the same slot race. */
 int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, int32_t heads,
                       const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v,
                       int64_t ld_v, const void* q_norm, const void* k_norm, float eps,
@@ -431,7 +431,8 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
  * lopa_paged_attention_workspace gives for the same sizes, NULL if that is 0.
  * Errors: LOPA_ECAPACITY for max_len > table_ld * page_size, LOPA_ESHAPE for a
  * layout the kernels do not take, too small a workspace, or more work than a launch
- * holds (never where rows * heads / 128 + n_seq * kv_heads < 2^24). */
+ * holds (never where rows * heads / 128 + n_seq * kv_heads < 2^24), LOPA_EINVAL for
+ * q and out that share memory. */
 int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch, int32_t heads,
                          int32_t max_rows, int32_t max_len, const void* q, int64_t ld_q,
                          int32_t block, float scale, float softcap, void* out, int64_t ld_out,

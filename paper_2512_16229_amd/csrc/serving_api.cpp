@@ -65,6 +65,29 @@ int check_rows(const char* name, const void* p, int64_t ld, int32_t heads, int32
   return LOPA_OK;
 }
 
+// Whether two arrays of `rows` rows of 2-byte elements share one: w_a elements each ld_a apart, and
+// w_b each ld_b apart. Views of one buffer may interleave without sharing.
+bool share(const void* a, int64_t ld_a, int64_t w_a, const void* b, int64_t ld_b, int64_t w_b, int64_t rows) {
+  const int64_t d = ((intptr_t)b - (intptr_t)a) / 2;  // both 16-byte aligned
+  if (d >= (rows - 1) * ld_a + w_a || -d >= (rows - 1) * ld_b + w_b) return false;
+  if (rows == 1) return true;
+  if (ld_a == ld_b) {  // row i of a and row i + k of b, |k| < rows: -w_b < d + k ld < w_a
+    const auto floor_div = [&](int64_t n) { return n / ld_a - (n % ld_a < 0); };
+    const int64_t lo = floor_div(-w_b - d) + 1, hi = floor_div(w_a - 1 - d);
+    return (lo > 1 - rows ? lo : 1 - rows) <= (hi < rows - 1 ? hi : rows - 1);
+  }
+  for (int64_t i = 0, j = 0; i < rows && j < rows;) {
+    const int64_t x = i * ld_a, y = d + j * ld_b;
+    if (x + w_a <= y)
+      ++i;
+    else if (y + w_b <= x)
+      ++j;
+    else
+      return true;
+  }
+  return false;
+}
+
 int launched(hipError_t e, const char* what) {
   return e == hipSuccess ? LOPA_OK : lopa_fail(LOPA_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
@@ -108,6 +131,10 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
   if (int e = check_rows("k", k, ld_k, pages->kv_heads, d)) return e;
   if (int e = check_rows("v", v, ld_v, pages->kv_heads, d)) return e;
   if (int e = check_rows("q_out", q_out, ld_out, heads, d)) return e;
+  const int64_t rows = batch->rows, wq = (int64_t)heads * d, wk = (int64_t)pages->kv_heads * d;
+  if (share(q_out, ld_out, wq, k, ld_k, wk, rows) || share(q_out, ld_out, wq, v, ld_v, wk, rows) ||
+      (!(q_out == q && (ld_out == ld_q || rows == 1)) && share(q_out, ld_out, wq, q, ld_q, wq, rows)))
+    return lopa_fail(LOPA_EINVAL, "q_out shares memory with k, v or other rows of q");
   AppendArgs a{};
   a.pages = *pages;
   a.batch = *batch;
@@ -162,6 +189,9 @@ int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch,
     if (!workspace || !aligned16(workspace))
       return lopa_fail(LOPA_EINVAL, "workspace null or not 16-byte aligned");
   }
+  // workgroups of other key splits read q while one writes out
+  if (share(q, ld_q, (int64_t)heads * d, out, ld_out, (int64_t)heads * d, batch->rows))
+    return lopa_fail(LOPA_EINVAL, "q and out share memory");
   PagedAttnArgs a{};
   a.pages = *pages;
   a.batch = *batch;

@@ -1,11 +1,12 @@
 """The serving operators at the edges of what their header promises."""
 import math
+import random
 
 import pytest
 import torch
 
 import serving_ref as ref
-from test_gpu_serving import BF, attend, randn
+from test_gpu_serving import BF, attend, randn, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +64,30 @@ def test_empty_batches(lp):
         f = lambda *s: torch.empty(s, device="cuda")
         lp.lopa_token_logprobs(f(0, 100), torch.empty(0, **i32), -1, f(0), f(0),
                                torch.empty((0, n), **i32), f(0, n))
+
+
+def test_views_of_one_buffer(lp):
+    """q and out as views of one buffer that interleave without sharing an element: the result of
+    separate arrays, and nothing else of the buffer changes."""
+    b = ref.Batch([(3, 40), (1, 700), (4, 4)], 16, 2, 64, BF, 3)
+    q = randn(5, (b.rows, 4, 64), BF)
+    want, _ = attend(lp, b, q)
+    ws = workspace(lp, 4, 2, 64, 3, b.rows, 4, 700)
+    rng, found, width = random.Random(4), 0, 256
+    for _ in range(400):
+        ld_q, ld_o = (8 * rng.randint(32, 150) for _ in range(2))
+        if rng.random() < 0.6:
+            ld_o = ld_q
+        at_q, at_o = (8 * rng.randint(0, 200) for _ in range(2))
+        if any(abs(at_q + i * ld_q - at_o - j * ld_o) < width for i in range(b.rows) for j in range(b.rows)):
+            continue
+        found += 1
+        store = torch.full((12000,), 7.0, dtype=BF, device="cuda")
+        view = lambda at, ld: store.as_strided((b.rows, 4, 64), (ld, 64, 1), at)
+        view(at_q, ld_q).copy_(q)
+        left = store.clone()
+        lp.lopa_paged_attention(view(at_q, ld_q), b.k, b.v, b.table, b.q_start, b.kv_len, 4, 700, 1, 0.125, 0.0,
+                                view(at_o, ld_o), None, ws)
+        left.as_strided((b.rows, 4, 64), (ld_o, 64, 1), at_o).copy_(want)
+        assert torch.equal(store, left), (ld_q, ld_o, at_q, at_o)
+    assert found > 50

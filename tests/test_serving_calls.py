@@ -2,6 +2,7 @@
 (pointers here are never dereferenced)."""
 import importlib.util
 import os
+import random
 
 import pytest
 import torch
@@ -76,3 +77,48 @@ def test_no_rows_need_no_arrays(lp):
     empty = dict(q=None, out=None, b=api.batch(lp, rows=0))
     assert api.attend(lp, **empty, ws=None, size=0) == 0 and api.append(lp, **empty, k=None, v=None) == 0
     assert api.logprobs(lp, rows=0, n=33) == -2 and api.logprobs(lp, rows=0, exclude=100) == -1
+
+
+# ----------------------------------------------------------------- shared memory
+# (rows, elements between the starts, row strides): heads of 64 elements, four of them
+SHARED = [(5, 0, 256, 256), (5, 128, 256, 256), (5, -128, 256, 256), (5, 4 * 256 + 248, 256, 256),
+          (5, 1000, 1024, 1024 + 8), (1, 248, 4096, 256), (3, 2 * 1024, 1024, 1024), (5, 1024 + 248, 512, 512),
+          (5, 3 * 512, 512, 2048), (7, -3 * 512 - 8, 2048, 512)]
+
+
+@pytest.mark.parametrize("rows,shift,ld_a,ld_b", SHARED)
+def test_shared_memory_is_refused(lp, rows, shift, ld_a, ld_b):
+    """Attention reads q in several workgroups while others write out, and append reads a row's keys
+    and values in other wavefronts than those that write its queries."""
+    a, b = 0x100000, 0x100000 + 2 * shift
+    batch = api.batch(lp, rows=rows)
+    kw = dict(b=batch, max_rows=rows)
+    assert api.attend(lp, q=a, ldq=ld_a, out=b, ldo=ld_b, **kw) == -1
+    assert b"share memory" in lp.lib.lopa_last_error()
+    assert api.attend(lp, q=b, ldq=ld_b, out=a, ldo=ld_a, **kw) == -1
+    far = dict(heads=4, p=api.pages(lp, kv_heads=4), b=batch)
+    x, y, z = 0x10000000, 0x20000000, 0x30000000
+    assert api.append(lp, q=x, k=a, ldk=ld_a, v=z, ldv=256, out=b, ldo=ld_b, **far) == -1
+    assert b"shares memory" in lp.lib.lopa_last_error()
+    assert api.append(lp, q=x, k=y, ldk=256, v=b, ldv=ld_b, out=a, ldo=ld_a, **far) == -1
+    if shift or (ld_a != ld_b and rows > 1):
+        assert api.append(lp, q=a, ldq=ld_a, k=y, ldk=256, v=z, ldv=256, out=b, ldo=ld_b, **far) == -1
+
+
+def test_shared_memory_is_refused_anywhere(lp):
+    """Views of one buffer at random places, against a search of all pairs of rows."""
+    rng, found = random.Random(3), 0
+    for _ in range(4000):
+        rows, shift = rng.randint(1, 9), 8 * rng.randint(-500, 500)
+        ld_a, ld_b = (8 * rng.randint(32, 150) for _ in range(2))
+        if rng.random() < 0.5:
+            ld_b = ld_a
+        if any(abs(i * ld_a - shift - j * ld_b) < 256 for i in range(rows) for j in range(rows)):
+            found += 1
+            assert api.attend(lp, q=0x100000, ldq=ld_a, out=0x100000 + 2 * shift, ldo=ld_b, max_rows=rows,
+                              b=api.batch(lp, rows=rows)) == -1, (rows, shift, ld_a, ld_b)
+    assert found > 1000
+
+
+def test_shared_memory_in_place_with_another_stride(lp):
+    assert api.append(lp, q=0x100000, ldq=256, k=0x20000000, v=0x30000000, out=0x100000, ldo=264) == -1
