@@ -417,6 +417,7 @@ int lopa_paged_append(const lopa_pages* pages, const lopa_paged_batch* batch, in
  *   block = c: j < (p / c + 1) c     block-causal: its own block and all before
  * (and j < kv_len always).
  *   s_j = scale q . K_j, or softcap tanh(scale q . K_j / softcap) if softcap > 0
+ *   (|scale|, softcap, 1 / softcap and |scale| / softcap at most 2^100)
  *   out = sum_j softmax(s)_j V_j;  lse = ln sum_j exp(s_j) (fp32 [rows][heads], or
  *   NULL)
  * A row that sees no key gives zeros and lse = -inf. Keys that a row does not see

@@ -16,6 +16,9 @@ constexpr int32_t MAX_SEQ = 65535;
 constexpr int32_t MAX_BATCH_ROWS = 1 << 24;
 constexpr int32_t MAX_HEADS = 1024;
 constexpr int32_t MAX_VOCAB = 1 << 24;
+// Factors of a score: in units of log2, and in those of the cap, a score of 0 stays 0 and no factor
+// is infinite.
+constexpr float MAX_FACTOR = 0x1p100f;
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -169,9 +172,10 @@ int lopa_paged_attention(const lopa_pages* pages, const lopa_paged_batch* batch,
   if (int e = check_paged(pages, batch, heads)) return e;
   if (int e = check_bounds(heads, batch->n_seq, batch->rows, max_rows, max_len)) return e;
   if (block < 0) return lopa_fail(LOPA_EINVAL, "block %d negative (0 full, 1 causal, c block-causal)", block);
-  if (!std::isfinite(scale)) return lopa_fail(LOPA_EINVAL, "scale must be finite");
-  if (!(softcap >= 0.f && std::isfinite(softcap)))
-    return lopa_fail(LOPA_EINVAL, "softcap must be finite and not negative (0: none)");
+  if (!(std::fabs(scale) <= MAX_FACTOR)) return lopa_fail(LOPA_EINVAL, "scale outside [-2^100, 2^100]");
+  if (softcap != 0.f && !(softcap >= 1 / MAX_FACTOR && softcap <= MAX_FACTOR &&
+                          std::fabs(scale) / softcap <= MAX_FACTOR))
+    return lopa_fail(LOPA_EINVAL, "softcap, 1 / softcap or |scale| / softcap outside [0, 2^100] (softcap 0: none)");
   if (batch->rows == 0 || batch->n_seq == 0 || max_rows == 0) return LOPA_OK;
   if (max_len > (int64_t)batch->table_ld * pages->page_size)
     return lopa_fail(LOPA_ECAPACITY, "max_len %d exceeds the table's %lld positions", max_len,

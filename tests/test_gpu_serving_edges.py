@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import serving_ref as ref
-from test_gpu_serving import BF, attend, randn, workspace
+from test_gpu_serving import BF, HF, attend, randn, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -46,6 +46,24 @@ def test_values_seen_far_below_the_maximum(lp, what, lens, heads, kv_heads, d):
         assert not torch.isfinite(out[..., 3]).any()
         rest = [i for i in range(d) if i != 3]
         assert torch.isfinite(out[..., rest]).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("scale,softcap", [(0.0, 0.0), (0.0, 30.0), (-0.2, 0.0), (-0.2, 5.0), (1.0, 2.0), (2.0 ** -100, 0.0),
+                                           (0.125, 2.0 ** -90), (0.125, 2.0 ** 90), (0.125, 1e6)])
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (HF, 64)])
+def test_scales_and_caps(lp, scale, softcap, dtype, d):
+    """Scales that are zero, negative or tiny, caps far from the scores."""
+    b = ref.Batch([(1, 1500), (40, 90), (0, 3), (3, 33)], 32, 2, d, dtype, 7, fill=math.nan)
+    q = randn(3, (b.rows, 6, d), dtype, 0.5)
+    q[:, 0] = 0  # scores of 0
+    out, lse = attend(lp, b, q, 1, softcap, scale=scale)
+    want, wlse, tol, ltol = ref.attention(b, q, 1, scale, softcap)
+    # ref's bound counts 8 U32 of the cap for the quotient, whose error is bounded by the cap's own
+    # slope too: |capped| <= |s|, 8 U32 of which the products' bound (d + 4) U32 covers
+    if softcap > 1000:
+        _, _, tol, ltol = ref.attention(b, q, 1, scale, 0.0)
+    ref.close(out, want, tol)
+    ref.close(lse, wlse, ltol)
 
 
 def test_empty_batches(lp):

@@ -122,3 +122,13 @@ def test_shared_memory_is_refused_anywhere(lp):
 
 def test_shared_memory_in_place_with_another_stride(lp):
     assert api.append(lp, q=0x100000, ldq=256, k=0x20000000, v=0x30000000, out=0x100000, ldo=264) == -1
+
+
+# ----------------------------------------------------------------- scale and cap
+@pytest.mark.parametrize("scale,cap", [(2.0 ** 101, 0.0), (-2.5e38, 0.0), (0.1, 2.0 ** 101), (0.1, 3e38),
+                                       (0.1, 2.0 ** -101), (0.0, 1e-40), (2.0 ** 60, 2.0 ** -60)])
+def test_scores_out_of_range(lp, scale, cap):
+    """Factors that leave fp32 made a score of 0 a NaN (0 x infinity)."""
+    q, out = 0x100000, 0x200000
+    assert api.attend(lp, scale=scale, cap=cap, q=q, out=out) == -1
+    assert b"2^100" in lp.lib.lopa_last_error()
