@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "attn_span.h"
+#include "paged_plan.h"
 #include "plan.h"
 
 #include "../../include/lopa.h"
@@ -196,9 +197,6 @@ struct AttnArgs {
 hipError_t launch_attention(const AttnArgs& a, hipStream_t s);
 
 // ------------------------------------------------- serving: paged cache
-// workgroups of 256 threads that a launch can have: its grid is counted in 32-bit work-items
-constexpr int64_t MAX_GROUPS = ((int64_t)1 << 24) - 1;
-
 struct AppendArgs {
   lopa_pages pages;
   lopa_paged_batch batch;
@@ -214,22 +212,6 @@ struct AppendArgs {
 };
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
 
-struct PagedPlan {
-  struct Part {           // one launch: the sequences with m_lo < rows x group <= m_hi
-    int wm;               // 32 wm rows a workgroup
-    int64_t m_lo, m_hi;
-    bool single;          // no sequence has more than one row tile
-    int64_t slots;        // row tiles' places
-    int splits, chunk;    // key splits of `chunk` keys
-    int64_t ws_bytes;
-    double us;            // expected
-  } part[2];
-  int n;
-  int64_t bytes;  // workspace of all parts
-  bool fits;      // no launch has more than MAX_GROUPS workgroups
-};
-PagedPlan paged_attention_plan(int heads, int kv_heads, int d, int n_seq, int rows, int max_rows,
-                               int max_len);
 struct PagedAttnArgs {
   lopa_pages pages;
   lopa_paged_batch batch;

@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import serving_ref as ref
-from test_gpu_serving import BF, HF, attend, randn, workspace
+from test_paged_plan import FORMS
+from test_gpu_serving import BF, HF, VARIANTS, attend, check_attend, randn, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -46,6 +47,29 @@ def test_values_seen_far_below_the_maximum(lp, what, lens, heads, kv_heads, d):
         assert not torch.isfinite(out[..., 3]).any()
         rest = [i for i in range(d) if i != 3]
         assert torch.isfinite(out[..., rest]).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,page,block,softcap", [(BF, 64, 1, 0.0), (HF, 32, 7, 0.0), (BF, 16, 0, 20.0),
+                                                      (HF, 128, 1, 20.0)])
+def test_attention_forms(lp, form, dtype, page, block, softcap):
+    """Every kernel form that a batch's sizes can choose (the launches are checked on the host by the
+    same table), in both types, with and without a cap."""
+    lens, heads, kv_heads, d, _ = FORMS[form]
+    b = ref.Batch(lens, page, kv_heads, d, dtype, 41, fill=math.nan)
+    q = randn(8, (b.rows, heads, d), dtype, 1.5)
+    check_attend(lp, b, q, block, softcap)
+
+
+@pytest.mark.parametrize("shape", VARIANTS)
+@pytest.mark.parametrize("dtype,page,block,softcap", [(HF, 16, 1, 20.0), (BF, 128, 32, 0.0)])
+def test_attention_variants_without_tail(lp, shape, dtype, page, block, softcap):
+    """The shapes of test_attention_variants without rows behind the last sequence, which make other
+    launches of some of them."""
+    lens, heads, kv_heads, d = VARIANTS[shape]
+    b = ref.Batch(lens, page, kv_heads, d, dtype, 33, fill=math.nan)
+    q = randn(9, (b.rows, heads, d), dtype, 1.5)
+    check_attend(lp, b, q, block, softcap)
 
 
 @pytest.mark.parametrize("scale,softcap", [(0.0, 0.0), (0.0, 30.0), (-0.2, 0.0), (-0.2, 5.0), (1.0, 2.0), (2.0 ** -100, 0.0),
