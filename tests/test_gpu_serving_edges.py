@@ -7,7 +7,7 @@ import torch
 
 import serving_ref as ref
 from test_paged_plan import FORMS
-from test_gpu_serving import BF, HF, VARIANTS, attend, check_attend, randn, workspace
+from test_gpu_serving import BF, HF, VARIANTS, attend, check_attend, randn, score, workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,52 @@ def test_views_of_one_buffer(lp):
         left.as_strided((b.rows, 4, 64), (ld_o, 64, 1), at_o).copy_(want)
         assert torch.equal(store, left), (ld_q, ld_o, at_q, at_o)
     assert found > 50
+
+
+# -------------------------------------------------------------------- logprobs
+def logprob_bounds(x, exclude):
+    """What the kernel's arithmetic allows (logprob, entropy and the 64-bit mean and variance behind
+    them), with U = 2^-24:
+    * a term 2^d, d = x log2 e - r, is off by |d| ln 2 U from the rounding of d, by a step (2 U) from
+      the exponential and |d| U from that of log2 e; each change of reference multiplies by a power
+      rounded like a term and rounds the product: 4 U, and once more |d| ln 2 U, all changes together
+      (they add up to at most |d|). There are at most the segments' changes and 4 of the joins.
+    * sums: 32 terms of a segment, the segments, 6 + 4 + 6 + 4 steps of the joins.
+    So S is off by (K + 3 E|d|) U relative, d in nats. The sum of d 2^d has these errors times |d|,
+      and 2 |d| U and 3 |d| U more for the products and for d; over S, whose error comes once more:
+      K (1 + 2 E|d|) + 8 E|d| + 6 E d^2.
+    * ln S and the value's own difference add 8 U of their size each."""
+    x = x.double().clone()
+    if exclude >= 0:
+        x[:, exclude] = -math.inf
+    V = x.shape[1]
+    m = x.amax(1, keepdim=True)
+    e = torch.exp(x - m)
+    p = e / e.sum(1, keepdim=True)
+    dist = torch.where(p > 0, m - x, 0.0)
+    mean, square = (p * dist).sum(1), (p * dist * dist).sum(1)
+    segments = V // 4096 + 5  # 1024 vectors a segment, of 4 elements at least
+    K = 32 + segments + 20 + 4 * (segments + 4) + 4
+    U = ref.U32
+    return (K + 3 * mean) * U, (K * (1 + 2 * mean) + 8 * mean + 6 * square) * U
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, torch.float32])
+@pytest.mark.parametrize("rows,vocab,std,shift", [(3, 1000, 1.0, 0.0), (2, 152064, 3.0, 0.0), (300, 8191, 3.0, 50.0),
+                                                  (40, 30000, 0.01, -500.0), (1100, 20001, 8.0, 3.0)])
+def test_logprobs_accuracy(lp, dtype, rows, vocab, std, shift):
+    """Within what the sums' depths allow: some 1e-5, not the order of any sum of the row's terms."""
+    x = (randn(vocab, (rows, vocab), torch.float32, std) + shift).to(dtype)
+    tokens = torch.randint(0, vocab, (rows,), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    tokens = tokens.to(torch.int32)
+    tokens[::2] = x[::2].float().argmax(1).to(torch.int32)
+    n, exclude = 8, vocab // 3
+    tokens[tokens == exclude] = 0
+    lo, en, ids, tl = score(lp, x, tokens, exclude, n)
+    wl, we, wi, wt, _ = ref.logprobs(x, tokens, exclude, n)
+    bound, ebound = logprob_bounds(x, exclude)
+    assert bound.max() < 5e-5
+    assert torch.equal(ids, wi)
+    ref.close(lo, wl, bound + 8 * ref.U32 * wl.abs())
+    ref.close(tl, wt, bound[:, None] + 8 * ref.U32 * wt.abs())
+    ref.close(en, we, ebound + 8 * ref.U32 * we.abs())
