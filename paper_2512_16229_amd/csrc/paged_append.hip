@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(64 * WAVES) paged_append_kernel(AppendArgs a, 
   const int s = seq_of_row(a.batch.q_start, a.batch.n_seq, row);
   if (s < 0) return;
   const int start = a.batch.q_start[s], end = a.batch.q_start[s + 1];
-  if (start < 0 || row >= end || end > a.batch.rows) return;
+  if (start < 0 || row < start || row >= end || end > a.batch.rows) return;
   const int64_t pos64 = (int64_t)a.batch.kv_len[s] - (end - row);
   const int pos = pos64 < INT32_MIN ? INT32_MIN : (int)pos64;
   // first element of this row's slot in head 0 of its page; < 0: no page

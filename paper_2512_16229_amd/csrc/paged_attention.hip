@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(256, WM == 4 ? 2 : 1) attn_kernel(PagedAttnArg
   if (!read_seq(a, s, q)) return;
   if (!L.single) tile = slot - (int)((int64_t)q.start * G / BM + s);
   const int64_t M = (int64_t)q.n * G;
-  if (M <= L.m_lo || M > L.m_hi || (int64_t)tile * BM >= M) return;
+  if (M <= L.m_lo || M > L.m_hi || tile < 0 || (int64_t)tile * BM >= M) return;  // tile < 0: q_start out of order
   const int m0 = tile * BM, m1 = (int)(M < m0 + BM ? M : m0 + BM);  // this tile's rows
   const int pos0 = q.len - q.n;
   const int lim_tile = key_limit(pos0 + (int)quotient(m1 - 1, L.group), L.block, q.len);
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(PagedAttnArgs a, JoinArg
   if (head >= a.heads) return;
   const int s = seq_of_row(a.batch.q_start, a.batch.n_seq, row);
   Seq q;
-  if (!read_seq(a, s, q) || row >= q.start + q.n) return;
+  if (!read_seq(a, s, q) || row < q.start || row >= q.start + q.n) return;
   const int Hkv = a.pages.kv_heads, G = j.l[0].group.d, kvh = quotient(head, j.l[0].group);
   const int64_t M = (int64_t)q.n * G;
   const int which = j.n > 1 && !(M > j.l[0].m_lo && M <= j.l[0].m_hi);

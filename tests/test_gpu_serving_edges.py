@@ -182,3 +182,46 @@ def test_logprobs_accuracy(lp, dtype, rows, vocab, std, shift):
     ref.close(lo, wl, bound + 8 * ref.U32 * wl.abs())
     ref.close(tl, wt, bound[:, None] + 8 * ref.U32 * wt.abs())
     ref.close(en, we, ebound + 8 * ref.U32 * we.abs())
+
+
+# ------------------------------------------------------------------- batch tables
+@pytest.mark.parametrize("starts", [[40, 0, 8, 20], [0, 40, 8, 20], [0, 8, 4, 20, 12, 30], [-3, 5, 60, 10], [0, 1, 30, 60, 2, 3],
+                                    [0, 2, 40, 70, 3, 4, 5]])
+@pytest.mark.parametrize("m", [100, 9000])
+def test_starts_out_of_order(lp, starts, m):
+    """q_start has to be in order. Where it is not the rows it names are undefined, but nothing lies
+    outside the arrays: rows past every start stay as they are, and so do pages of no table."""
+    n_seq, rows, hkv, d = len(starts) - 1, 70, 2, 64
+    b = ref.Batch([(1, m)] * n_seq, 16, hkv, d, BF, 5)
+    b.q_start = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    k0, v0 = b.k.clone(), b.v.clone()
+    q, kv = randn(3, (rows, 8, d), BF), randn(4, (rows, hkv, d), BF)
+    out = torch.full_like(q, 7.0)
+    ws = workspace(lp, 8, hkv, d, n_seq, rows, rows, m)
+    lp.lopa_paged_attention(q, b.k, b.v, b.table, b.q_start, b.kv_len, rows, m, 1, 0.125, 0.0, out, None, ws)
+    assert (out[max(starts):] == 7).all()
+    out.fill_(7.0)
+    lp.lopa_paged_append(b.k, b.v, b.table, b.q_start, b.kv_len, q, kv, kv, None, None, 0.0, 1e4, out)
+    assert (out[max(starts):] == 7).all()
+    free = torch.ones(b.k.shape[0], dtype=torch.bool, device="cuda")
+    free[b.table[b.table >= 0].long()] = False
+    assert free.any() and torch.equal(b.k[free], k0[free]) and torch.equal(b.v[free], v0[free])
+
+
+@pytest.mark.parametrize("form", ["64 rows", "tiles of 64, split", "tiles of 128", "tiles of 128, split, d 64",
+                                  "two launches"])
+def test_other_lengths_within_the_bounds(lp, form):
+    """The launches are laid out for rows, max_rows and max_len: a captured call serves every batch
+    within them. Here sequences shrink, empty and move, rows behind the last one stay."""
+    lens, heads, kv_heads, d, _ = FORMS[form]
+    rows, max_rows, max_len = sum(n for n, _ in lens), max(n for n, _ in lens), max(m for _, m in lens)
+    rng = random.Random(7)
+    for shrink in (1, 3, 40):
+        less = [(rng.randint(0, -(-n // shrink)), m) for n, m in lens]
+        less = [(n, rng.randint(n, m)) for n, m in less]
+        b = ref.Batch(less, 32, kv_heads, d, BF, 43, fill=math.nan)
+        pad = torch.full((len(lens), -(-max_len // 32)), -1, dtype=torch.int32, device="cuda")
+        pad[:, :b.table.shape[1]] = b.table[:, :pad.shape[1]]
+        b.table = pad
+        q = randn(10, (rows, heads, d), BF)
+        check_attend(lp, b, q, 1, max_rows=max_rows, max_len=max_len)
