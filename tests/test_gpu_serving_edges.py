@@ -225,3 +225,71 @@ def test_other_lengths_within_the_bounds(lp, form):
         b.table = pad
         q = randn(10, (rows, heads, d), BF)
         check_attend(lp, b, q, 1, max_rows=max_rows, max_len=max_len)
+
+
+# ---------------------------------------------------------------------- append
+@pytest.mark.parametrize("which", ["q", "k"])
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 2, 64), (5, 1, 128), (17, 17, 64)])
+def test_append_one_norm(lp, which, heads, kv_heads, d):
+    """A norm for the queries or the keys alone (heads of both kinds share a wavefront), the queries
+    written in place in the packed rows that the keys and values lie in too."""
+    b = ref.Batch([(5, 90), (0, 3), (1, 17)], 16, kv_heads, d, HF, 4)
+    qkv = randn(9, (b.rows + 2, heads + 2 * kv_heads, d), HF, 2.0)
+    before = qkv.clone()
+    q, k, v = qkv.split([heads, kv_heads, kv_heads], 1)
+    w = (1 + randn(1, (d,), torch.float32, 0.2)).to(HF)
+    norms = (w, None) if which == "q" else (None, w)
+    wq, tq, wk, tk = ref.append(b, q.clone(), k, v, *norms, 1e-6, 1e4)
+    lp.lopa_paged_append(b.k, b.v, b.table, b.q_start, b.kv_len, q, k, v, *norms, 1e-6, 1e4, q)
+    ref.close(q[:b.rows], wq, tq)
+    assert torch.equal(qkv[:, heads:], before[:, heads:]) and torch.equal(qkv[b.rows:], before[b.rows:])
+    for row, (s, p) in enumerate([(0, i) for i in range(85, 90)] + [(2, 16)]):
+        page = b.table[s, p // 16].long()
+        ref.close(b.k[page, :, p % 16], wk[row], tk[row])
+        assert torch.equal(b.v[page, :, p % 16], v[row])
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(1024, 1), (1024, 1024), (1024, 8), (1, 1)])
+def test_many_heads(lp, heads, kv_heads):
+    b = ref.Batch([(1, 40), (3, 5), (2, 600)], 32, kv_heads, 64, BF, 4, fill=math.nan)
+    q, kv = randn(3, (b.rows, heads, 64), BF, 1.5), randn(4, (b.rows, kv_heads, 64), BF)
+    out = torch.empty_like(q)
+    lp.lopa_paged_append(b.k, b.v, b.table, b.q_start, b.kv_len, q, kv, kv, None, None, 0.0, 1e4, out)
+    wq, tq, _, _ = ref.append(b, q, kv, kv, None, None, 0.0, 1e4)
+    ref.close(out, wq, tq)
+    check_attend(lp, b, q, 1)
+
+
+def test_shared_pages(lp):
+    """Branches of one prefix: the same pages in several tables, full and causal."""
+    n, m, ps = 3, 150, 32
+    b = ref.Batch([(9, m)] * n, ps, 2, 128, BF, 4, fill=math.nan)
+    share = (m - 9) // ps
+    b.table[1:, :share] = b.table[0, :share]
+    q = randn(3, (b.rows, 8, 128), BF)
+    for block in (0, 1):
+        out, _ = check_attend(lp, b, q, block)
+    q[9:] = q[:9].repeat(2, 1, 1)
+    for s in range(1, n):  # the same new tokens: the same answers
+        for p in range(share, -(-m // ps)):
+            b.k[b.table[s, p].long()], b.v[b.table[s, p].long()] = b.k[b.table[0, p].long()], b.v[b.table[0, p].long()]
+    out, lse = attend(lp, b, q, 1)
+    assert torch.equal(out[9:], out[:9].repeat(2, 1, 1)) and torch.equal(lse[9:], lse[:9].repeat(2, 1))
+
+
+def test_two_streams_at_once(lp):
+    """The same pages read by two streams, each with its own outputs and workspace."""
+    b = ref.Batch([(1, 5000), (40, 900)], 64, 2, 128, BF, 4)
+    q = randn(3, (b.rows, 8, 128), BF)
+    want = attend(lp, b, q)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [(torch.empty_like(q), torch.empty((b.rows, 8), device="cuda"),
+            workspace(lp, 8, 2, 128, 2, b.rows, 40, 5000)) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for st, (out, lse, ws) in zip(streams, got):
+            lp.lopa_paged_attention(q, b.k, b.v, b.table, b.q_start, b.kv_len, 40, 5000, 1, 128 ** -0.5, 0.0, out,
+                                    lse, ws, stream=st)
+    torch.cuda.synchronize()
+    for out, lse, _ in got:
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
